@@ -508,6 +508,86 @@ dp_status_t dp_clipped_grad_sum_positional_noised(const void* dE, int64_t lde, c
                                                   int B_norm, uint64_t seed, uint64_t step,
                                                   void* stream);
 
+/* ---------------------------------------------------------------------
+ * LayerNorm of every token, y = gain * xhat + bias with
+ *   xhat = (x - mean) * rstd, rstd = 1 / sqrt(variance + eps)
+ * over the d features of a row (the variance divides by d). x and y are
+ * [B,T,d] (dt; row strides ldx, ldy; y may be x); gain and bias are device
+ * arrays of d elements of param_dt (NULL: 1 and 0). mean and rstd (fp32
+ * [B*T], either may be NULL) are what the backward pass needs.
+ * Statistics are fp32. d <= 32768 (else DP_EUNSUPPORTED), B*T < 2^31. Rows of
+ * any alignment; operands may span more than 4 GiB.
+ * ------------------------------------------------------------------- */
+dp_status_t dp_layernorm_forward(const void* x, int64_t ldx, const void* gain, const void* bias,
+                                 dp_dtype_t param_dt, int B, int T, int d, dp_dtype_t dt,
+                                 float eps, void* y, int64_t ldy, float* mean, float* rstd,
+                                 void* stream);
+
+/* Its backward pass with the per-example gradients of gain and bias (the
+ * sums of dp_vector_grads_grouped, without xhat in memory): with g = gain*gy,
+ *   dx = (accumulate_dx ? dx : 0) + rstd (g - mean_f(g) - xhat mean_f(g xhat))
+ *   dgain[i,:] = sum_t gy[i,t] * xhat[i,t],  dbias[i,:] = sum_t gy[i,t]
+ *   norm2[i] = (accumulate ? norm2[i] : 0) + ||dgain[i]||^2 + ||dbias[i]||^2
+ * gy, x [B,T,d] (dt); mean, rstd as the forward pass wrote them; gain as there
+ * (used by dx only). dx [B,T,d] (dt) may be gy or x (with its row stride);
+ * dgain, dbias are fp32 [B,d], contiguous. dx, dgain, dbias and norm2 may be
+ * NULL; norm2 counts those of dgain and dbias that are given. For the sum over
+ * the whole batch instead, pass B = 1 and T = all tokens. Sums over tokens run
+ * in a fixed order (reproducible). Limits as above; the workspace is
+ * dp_layernorm_backward_workspace(B, T, d) bytes (0: none needed), 16-byte
+ * aligned, and unused when dgain and dbias are both NULL. */
+size_t dp_layernorm_backward_workspace(int B, int T, int d);
+dp_status_t dp_layernorm_backward(const void* gy, int64_t ldgy, const void* x, int64_t ldx,
+                                  const void* gain, dp_dtype_t param_dt, const float* mean,
+                                  const float* rstd, int B, int T, int d, dp_dtype_t dt, void* dx,
+                                  int64_t lddx, int accumulate_dx, float* dgain, float* dbias,
+                                  float* norm2, int accumulate, void* workspace,
+                                  size_t workspace_bytes, void* stream);
+
+/* ---------------------------------------------------------------------
+ * Losses of the head. Z [B,T,V] (dt, row stride ldz) are logits, targets
+ * int32 [B,T] the token each row is scored on; a target outside [0, V) marks
+ * a row that is not scored (a prompt's token, padding): it is not read, its
+ * log-probability is 0 and its gradient row zero. Elements of a gradient row
+ * past V are left as they are.
+ *   lse = log sum_v exp(Z[v]),  logp = Z[target] - lse        (fp32)
+ * -inf logits have probability 0; a scored row of nothing else has logp = lse
+ * = -inf and a zero gradient. NaN or +inf among a row's logits makes its
+ * outputs NaN, which dp_clip_factors answers with c = 0.
+ * V <= 2^30 (else DP_EUNSUPPORTED), B*T < 2^31; rows of any alignment;
+ * operands may span more than 4 GiB.
+ * ------------------------------------------------------------------- */
+/* logp [B,T] and (may be NULL) lse [B,T] (0 for rows that are not scored). */
+dp_status_t dp_token_logprobs(const void* Z, int64_t ldz, const int32_t* targets, int B, int T,
+                              int V, dp_dtype_t dt, float* logp, float* lse, void* stream);
+
+/* Cross-entropy, sum_t w[b,t] (-logp[b,t]) per example, and its gradient in
+ * one pass: Gz[b,t,:] = w[b,t] (softmax(Z[b,t,:]) - onehot(target)), the G
+ * operand of the head (dt, row stride ldg >= V; may be Z with its row stride).
+ * w is fp32 [B,T] (1/T for a mean over tokens); a row of weight 0 has a zero
+ * gradient whatever its logits hold. logp [B,T] may be NULL. */
+dp_status_t dp_cross_entropy(const void* Z, int64_t ldz, const int32_t* targets, const float* w,
+                             int B, int T, int V, dp_dtype_t dt, float* logp, void* Gz,
+                             int64_t ldg, void* stream);
+
+/* Preference loss of pairs of answers: an example is a pair, tokens t < split
+ * the chosen answer (its prompt not scored), t >= split the rejected one, so
+ * that a pair's gradient is clipped as a whole. With the log-probabilities
+ * ref_logp [B,T] of a frozen reference model (NULL: none, all 0)
+ *   rewards[b] = beta (sum over an answer's scored tokens of logp - ref_logp)
+ *   m = rewards[b,0] - rewards[b,1]
+ *   loss[b] = -(1 - label_smoothing) log sigma(m) - label_smoothing log sigma(-m)
+ * and Gz = d loss / d Z (as for dp_cross_entropy; NULL: the loss alone).
+ * rewards [B,2] and logp [B,T] may be NULL. beta > 0, 0 <= label_smoothing < 0.5.
+ * Sums over tokens are in double, in a fixed order. The workspace is
+ * dp_preference_loss_workspace(B, T) bytes, 16-byte aligned. */
+size_t dp_preference_loss_workspace(int B, int T);
+dp_status_t dp_preference_loss(const void* Z, int64_t ldz, const int32_t* targets, int split,
+                               const float* ref_logp, float beta, float label_smoothing, int B,
+                               int T, int V, dp_dtype_t dt, float* loss, float* rewards,
+                               float* logp, void* Gz, int64_t ldg, void* workspace,
+                               size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

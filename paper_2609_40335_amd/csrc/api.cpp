@@ -1460,3 +1460,5 @@ dp_status_t dp_clipped_grad_sum_positional_noised(const void* dE, int64_t lde, c
 }
 
 }  // extern "C"
+
+#include "api_step.hpp"

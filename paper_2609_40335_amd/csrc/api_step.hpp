@@ -1,0 +1,212 @@
+// C ABI of the operators on either side of the norms and sums: LayerNorm, the
+// head's losses, orthogonalised updates (part of api.cpp, whose helpers it uses).
+#pragma once
+
+namespace {
+
+// Rows of w elements, ld apart, of a matrix of B*T rows.
+dp_status_t check_rows(int B, int T, int w, dp_dtype_t dt, const char* width) {
+  if (B <= 0 || T <= 0 || w <= 0) return fail(DP_EINVAL, "B, T and %s must be positive", width);
+  if (!dtype_ok(dt)) return fail(DP_EINVAL, "unknown dtype %d", (int)dt);
+  if ((int64_t)B * T > INT32_MAX)
+    return fail(DP_EUNSUPPORTED, "B*T = %lld exceeds 2^31 - 1", (long long)((int64_t)B * T));
+  return DP_OK;
+}
+
+struct LnWorkspace {
+  dpg::LnPlan plan;
+  size_t sq, total;  // offset of the partial squares; bytes in all
+};
+LnWorkspace ln_workspace(int B, int T, int d) {
+  LnWorkspace w;
+  w.plan = dpg::ln_plan(B, T, d, true);
+  w.sq = w.total = 0;
+  if (w.plan.ranges > 1) {
+    w.sq = align_up((size_t)B * w.plan.ranges * 2 * (size_t)d * 4);
+    w.total = w.sq + align_up((size_t)B * w.plan.chunks * 4);
+  }
+  return w;
+}
+
+// Preference loss scratch: log p (double), statistics and slopes of the rows.
+struct PrefLayout {
+  size_t stat, slope, total;
+};
+PrefLayout pref_layout(int B, int T) {
+  const size_t rows = (size_t)B * T;
+  PrefLayout l;
+  l.stat = align_up(rows * 8);
+  l.slope = l.stat + align_up(rows * sizeof(dpg::RowStat));
+  l.total = l.slope + align_up((size_t)B * 4);
+  return l;
+}
+
+constexpr int MAX_LOGITS = 1 << 30;  // columns are counted in 32 bits
+
+dp_status_t check_logits(const void* Z, int64_t ldz, const int32_t* targets, int B, int T, int V,
+                         dp_dtype_t dt) {
+  if (!Z || !targets) return fail(DP_EINVAL, "Z or targets is NULL");
+  dp_status_t st = check_rows(B, T, V, dt, "V");
+  if (st != DP_OK) return st;
+  if (V > MAX_LOGITS) return fail(DP_EUNSUPPORTED, "V = %d exceeds 2^30", V);
+  if (ldz < V) return fail(DP_EINVAL, "ldz < V");
+  return DP_OK;
+}
+
+// The gradient may replace the logits, but not overlap them in another layout.
+dp_status_t check_in_place(const void* Z, int64_t ldz, const void* Gz, int64_t ldg) {
+  if (Gz == Z && ldg != ldz) return fail(DP_EINVAL, "in place, ldg must equal ldz");
+  return DP_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+dp_status_t dp_layernorm_forward(const void* x, int64_t ldx, const void* gain, const void* bias,
+                                 dp_dtype_t param_dt, int B, int T, int d, dp_dtype_t dt,
+                                 float eps, void* y, int64_t ldy, float* mean, float* rstd,
+                                 void* stream) {
+  if (!x || !y) return fail(DP_EINVAL, "x or y is NULL");
+  dp_status_t st = check_rows(B, T, d, dt, "d");
+  if (st != DP_OK) return st;
+  if (!dtype_ok(param_dt)) return fail(DP_EINVAL, "unknown dtype %d", (int)param_dt);
+  if (d > dpg::LN_MAX_D) return fail(DP_EUNSUPPORTED, "d = %d exceeds %d", d, dpg::LN_MAX_D);
+  if (ldx < d || ldy < d) return fail(DP_EINVAL, "row stride smaller than d");
+  if (!(eps >= 0.f) || !std::isfinite(eps)) return fail(DP_EINVAL, "eps must be >= 0");
+  if (y == x && ldy != ldx) return fail(DP_EINVAL, "in place, ldy must equal ldx");
+  dpg::LnForwardArgs a{};
+  a.x = x; a.gain = gain; a.bias = bias; a.y = y; a.mean = mean; a.rstd = rstd;
+  a.ldx = ldx; a.ldy = ldy; a.rows = (int64_t)B * T;
+  a.d = d; a.param_dt = kdt(param_dt); a.eps = eps;
+  return hip_status(dpg::launch_ln_forward(a, kdt(dt), as_stream(stream)), "layernorm launch");
+}
+
+size_t dp_layernorm_backward_workspace(int B, int T, int d) {
+  if (B <= 0 || T <= 0 || d <= 0 || d > dpg::LN_MAX_D) return 0;
+  return ln_workspace(B, T, d).total;
+}
+
+dp_status_t dp_layernorm_backward(const void* gy, int64_t ldgy, const void* x, int64_t ldx,
+                                  const void* gain, dp_dtype_t param_dt, const float* mean,
+                                  const float* rstd, int B, int T, int d, dp_dtype_t dt, void* dx,
+                                  int64_t lddx, int accumulate_dx, float* dgain, float* dbias,
+                                  float* norm2, int accumulate, void* workspace,
+                                  size_t workspace_bytes, void* stream) {
+  if (!gy || !x || !mean || !rstd) return fail(DP_EINVAL, "gy, x, mean or rstd is NULL");
+  if (!dx && !dgain && !dbias) return fail(DP_EINVAL, "dx, dgain and dbias are all NULL");
+  if (norm2 && !dgain && !dbias)
+    return fail(DP_EINVAL, "norm2 is the squared norm of dgain and dbias: both are NULL");
+  dp_status_t st = check_rows(B, T, d, dt, "d");
+  if (st != DP_OK) return st;
+  if (!dtype_ok(param_dt)) return fail(DP_EINVAL, "unknown dtype %d", (int)param_dt);
+  if (d > dpg::LN_MAX_D) return fail(DP_EUNSUPPORTED, "d = %d exceeds %d", d, dpg::LN_MAX_D);
+  if (ldgy < d || ldx < d || (dx && lddx < d)) return fail(DP_EINVAL, "row stride smaller than d");
+  if (dx && ((dx == gy && lddx != ldgy) || (dx == x && lddx != ldx)))
+    return fail(DP_EINVAL, "in place, lddx must equal the operand's row stride");
+  const bool grads = dgain || dbias;
+  dpg::LnBackwardArgs a{};
+  LnWorkspace w{dpg::ln_plan(B, T, d, false), 0, 0};
+  if (grads) w = ln_workspace(B, T, d);
+  if (w.total) {
+    if (!workspace || workspace_bytes < w.total)
+      return fail(DP_EINVAL, "workspace of %zu bytes needed", w.total);
+    if (!aligned16(workspace)) return fail(DP_EINVAL, "workspace must be 16-byte aligned");
+    a.ws = static_cast<float*>(workspace);
+    a.sq = reinterpret_cast<float*>(static_cast<char*>(workspace) + w.sq);
+  }
+  a.gy = gy; a.x = x; a.gain = gain; a.mean = mean; a.rstd = rstd;
+  a.dx = dx; a.dgain = dgain; a.dbias = dbias; a.norm2 = norm2;
+  a.ldgy = ldgy; a.ldx = ldx; a.lddx = lddx;
+  a.B = B; a.T = T; a.d = d; a.param_dt = kdt(param_dt);
+  a.ranges = w.plan.ranges; a.span = w.plan.span; a.chunks = w.plan.chunks;
+  a.accumulate_dx = accumulate_dx ? 1 : 0; a.accumulate = accumulate ? 1 : 0;
+  return hip_status(dpg::launch_ln_backward(a, kdt(dt), as_stream(stream)),
+                    "layernorm backward launch");
+}
+
+dp_status_t dp_token_logprobs(const void* Z, int64_t ldz, const int32_t* targets, int B, int T,
+                              int V, dp_dtype_t dt, float* logp, float* lse, void* stream) {
+  dp_status_t st = check_logits(Z, ldz, targets, B, T, V, dt);
+  if (st != DP_OK) return st;
+  if (!logp) return fail(DP_EINVAL, "logp is NULL");
+  dpg::LossArgs a{};
+  a.Z = Z; a.ldz = ldz; a.targets = targets; a.logp = logp; a.lse = lse;
+  a.rows = (int64_t)B * T; a.V = V; a.T = T;
+  return hip_status(dpg::launch_token_logprobs(a, kdt(dt), as_stream(stream)),
+                    "token_logprobs launch");
+}
+
+dp_status_t dp_cross_entropy(const void* Z, int64_t ldz, const int32_t* targets, const float* w,
+                             int B, int T, int V, dp_dtype_t dt, float* logp, void* Gz,
+                             int64_t ldg, void* stream) {
+  dp_status_t st = check_logits(Z, ldz, targets, B, T, V, dt);
+  if (st != DP_OK) return st;
+  if (!w || !Gz) return fail(DP_EINVAL, "w or Gz is NULL");
+  if (ldg < V) return fail(DP_EINVAL, "ldg < V");
+  st = check_in_place(Z, ldz, Gz, ldg);
+  if (st != DP_OK) return st;
+  dpg::LossArgs a{};
+  a.Z = Z; a.ldz = ldz; a.targets = targets; a.w = w; a.logp = logp; a.Gz = Gz; a.ldg = ldg;
+  a.rows = (int64_t)B * T; a.V = V; a.T = T;
+  return hip_status(dpg::launch_cross_entropy(a, kdt(dt), as_stream(stream)),
+                    "cross_entropy launch");
+}
+
+size_t dp_preference_loss_workspace(int B, int T) {
+  if (B <= 0 || T <= 0) return 0;
+  return pref_layout(B, T).total;
+}
+
+dp_status_t dp_preference_loss(const void* Z, int64_t ldz, const int32_t* targets, int split,
+                               const float* ref_logp, float beta, float label_smoothing, int B,
+                               int T, int V, dp_dtype_t dt, float* loss, float* rewards,
+                               float* logp, void* Gz, int64_t ldg, void* workspace,
+                               size_t workspace_bytes, void* stream) {
+  dp_status_t st = check_logits(Z, ldz, targets, B, T, V, dt);
+  if (st != DP_OK) return st;
+  if (!loss) return fail(DP_EINVAL, "loss is NULL");
+  if (split < 0 || split > T) return fail(DP_EINVAL, "split = %d is not in [0, T]", split);
+  if (!(beta > 0.f) || !std::isfinite(beta)) return fail(DP_EINVAL, "beta must be positive");
+  if (!(label_smoothing >= 0.f) || !(label_smoothing < 0.5f))
+    return fail(DP_EINVAL, "label_smoothing must be in [0, 0.5)");
+  if (Gz) {
+    if (ldg < V) return fail(DP_EINVAL, "ldg < V");
+    st = check_in_place(Z, ldz, Gz, ldg);
+    if (st != DP_OK) return st;
+  }
+  const PrefLayout l = pref_layout(B, T);
+  if (!workspace || workspace_bytes < l.total)
+    return fail(DP_EINVAL, "workspace of %zu bytes needed", l.total);
+  if (!aligned16(workspace)) return fail(DP_EINVAL, "workspace must be 16-byte aligned");
+  char* ws = static_cast<char*>(workspace);
+  hipStream_t s = as_stream(stream);
+  dpg::LossArgs a{};
+  a.Z = Z; a.ldz = ldz; a.targets = targets; a.logp = logp; a.Gz = Gz; a.ldg = ldg;
+  a.logp64 = reinterpret_cast<double*>(ws);
+  a.stat = reinterpret_cast<dpg::RowStat*>(ws + l.stat);
+  a.w = reinterpret_cast<float*>(ws + l.slope);
+  a.V = V; a.T = T; a.split = split;
+  const int64_t pairs = dpg::preference_pairs(B, T, V, esize(dt));
+  for (int64_t b = 0; b < B; b += pairs) {
+    const int64_t n = std::min<int64_t>(pairs, B - b);
+    a.row0 = b * T;
+    a.rows = n * T;
+    st = hip_status(dpg::launch_token_logprobs(a, kdt(dt), s), "token_logprobs launch");
+    if (st != DP_OK) return st;
+    dpg::PreferenceArgs p{};
+    p.targets = targets + a.row0; p.logp = a.logp64 + a.row0;
+    p.ref = ref_logp ? ref_logp + a.row0 : nullptr;
+    p.loss = loss + b; p.rewards = rewards ? rewards + 2 * b : nullptr;
+    p.slope = reinterpret_cast<float*>(ws + l.slope) + b;
+    p.T = T; p.V = V; p.split = split; p.beta = beta; p.smoothing = label_smoothing;
+    st = hip_status(dpg::launch_preference(p, (int)n, s), "preference launch");
+    if (st != DP_OK) return st;
+    if (!Gz) continue;
+    st = hip_status(dpg::launch_logit_grads(a, kdt(dt), s), "logit_grads launch");
+    if (st != DP_OK) return st;
+  }
+  return DP_OK;
+}
+
+}  // extern "C"

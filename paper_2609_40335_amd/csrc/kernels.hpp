@@ -422,6 +422,102 @@ struct PosSumArgs {
 };
 hipError_t launch_pos_sum(const PosSumArgs& a, int dt, hipStream_t s);
 
+// ---------------------------------------------------------------- LayerNorm
+constexpr int LN_MAX_D = 32768;     // a row is held in the registers of at most 16 waves
+struct LnForwardArgs {
+  const void* x;        // [rows, ldx]
+  const void* gain;     // [d] of param_dt, or null (1)
+  const void* bias;     // [d] of param_dt, or null (0)
+  void* y;              // [rows, ldy]
+  float* mean;          // nullable [rows]
+  float* rstd;          // nullable [rows]
+  int64_t ldx, ldy, rows;
+  int32_t d, param_dt;
+  float eps;
+};
+hipError_t launch_ln_forward(const LnForwardArgs& a, int dt, hipStream_t s);
+
+struct LnBackwardArgs {
+  const void* gy;       // [B*T rows, ldgy]
+  const void* x;        // [B*T rows, ldx]
+  const void* gain;     // [d] of param_dt, or null (1)
+  const float* mean;    // [B*T]
+  const float* rstd;    // [B*T]
+  void* dx;             // nullable [B*T rows, lddx]
+  float* dgain;         // nullable [B, d]
+  float* dbias;         // nullable [B, d]
+  float* norm2;         // nullable [B]
+  float* ws;            // [B, ranges, 2, d] partial sums (ranges > 1)
+  float* sq;            // [B, chunks] partial squares (ranges > 1)
+  int64_t ldgy, ldx, lddx;
+  int32_t B, T, d, param_dt;
+  int32_t ranges, span; // an example's rows are cut into `ranges` of `span`
+  int32_t chunks;       // workgroups per example of the second launch
+  int32_t accumulate_dx, accumulate;
+};
+hipError_t launch_ln_backward(const LnBackwardArgs& a, int dt, hipStream_t s);
+
+// How the backward pass cuts an example's T rows: about LN_GROUPS workgroups in
+// all, but no fewer rows each than keep the partial sums' way to memory and back
+// (16 d bytes a range) below a quarter of the operands' (3 T d elements).
+constexpr int LN_GROUPS = 1024;
+struct LnPlan {
+  int32_t ranges, span, chunks;
+};
+inline LnPlan ln_plan(int B, int T, int d, bool grads) {
+  const int teams = d <= 2048 ? 8 : 1;
+  const int least = grads ? (teams > 1 ? 2 * teams : 8) : teams;
+  int64_t ranges = (LN_GROUPS + B - 1) / B, most = (T + least - 1) / least;
+  if (ranges > most) ranges = most;
+  LnPlan p;
+  p.span = (int32_t)((T + ranges - 1) / ranges);
+  p.ranges = (T + p.span - 1) / p.span;
+  // One workgroup per example adds up to this many partial sums itself.
+  p.chunks = (int64_t)p.ranges * d <= 16384 ? 1 : (d + 63) / 64;
+  return p;
+}
+
+// ------------------------------------------------------------------- losses
+struct RowStat {
+  float top, scale;     // largest logit; 1 / sum exp(z - top), 0 for a row without any
+};
+struct LossArgs {
+  const void* Z;        // [rows, ldz] logits
+  void* Gz;             // [rows, ldg] their gradient (may be Z)
+  const int32_t* targets;  // [rows]; outside [0, V): ignored
+  const float* w;       // [rows] weights (cross-entropy), or [B] (preference)
+  float* logp;          // nullable [rows]
+  float* lse;           // nullable [rows]
+  double* logp64;       // nullable [rows] (preference)
+  RowStat* stat;        // nullable [rows] (preference)
+  int64_t ldz, ldg, rows, row0;
+  int32_t V, T, split;  // split: tokens before it are the chosen answer's (preference)
+};
+// log p and its logarithmic sum of every row; with a.stat also what the backward pass needs.
+hipError_t launch_token_logprobs(const LossArgs& a, int dt, hipStream_t s);
+// log p and the weighted gradient in one pass over the logits.
+hipError_t launch_cross_entropy(const LossArgs& a, int dt, hipStream_t s);
+// The gradient from saved row statistics.
+hipError_t launch_logit_grads(const LossArgs& a, int dt, hipStream_t s);
+
+struct PreferenceArgs {
+  const int32_t* targets;  // [B, T]
+  const double* logp;   // [B, T]
+  const float* ref;     // nullable [B, T]
+  float* loss;          // [B]
+  float* rewards;       // nullable [B, 2]
+  float* slope;         // [B] -d loss / d log p of a chosen answer's token
+  int32_t T, V, split;
+  float beta, smoothing;
+};
+// Pairs of one pass: workgroups are counted in 32 bits.
+inline int64_t preference_pairs(int B, int T, int V, int es) {
+  (void)es;
+  const int64_t most = ((int64_t)1 << 30) / ((int64_t)T * ((V + 8191) / 8192));
+  return most < 1 ? 1 : most < B ? most : B;
+}
+hipError_t launch_preference(const PreferenceArgs& a, int B, hipStream_t s);
+
 // ----------------------------------------------------------- clip and noise
 // c (nullable) = clip factors; cs (nullable) = scale * clip factors; the
 // squared norm is norm2 (+ norm2_b when not null).

@@ -1,0 +1,325 @@
+// LayerNorm of every token and its backward pass with per-example gradients of
+// gain and bias (part of vector.hip).
+//
+// Forward: xhat = (x - mean) rstd, y = gain xhat + bias, with the mean and the
+// variance of the row's d features (the mean first, then the squares about it,
+// both from registers) and rstd = 1 / sqrt(variance + eps).
+// Backward, with g = gain gy: dx = rstd (g - mean(g) - xhat mean(g xhat)).
+// Example i's gradients are sums over its tokens, as for every vector parameter
+// here: dgain_i = sum_t gy xhat, dbias_i = sum_t gy (the chain rule of
+// vec_reduce_kernel, which wants xhat in memory; here it is formed from x and
+// the saved statistics), and the flat norm takes ||dgain_i||^2 + ||dbias_i||^2.
+//
+// Both passes are bound by HBM: 2 (forward) or 3 (backward) elements a feature.
+// A row is read once into the registers of a team, one wave up to 2048
+// features (its sums need no barrier), 4 waves up to 8192, 16 up to 32768, and
+// both sums of a row meet in one exchange. A lane holds the same features of
+// every row it meets, so the token sums of dgain and dbias stay in its
+// registers; a workgroup covers a range of an example's rows, and ranges are
+// added in order by a second launch (no atomics: results do not depend on
+// timing). One range per example needs none.
+#pragma once
+#include "rows.hpp"
+
+namespace dpg {
+
+constexpr int LN_WAVES = 8;   // waves of a workgroup whose teams are single waves
+
+template <int W>
+struct LnTeam {
+  static constexpr int THREADS = W == 1 ? LN_WAVES * WAVE : W * WAVE;
+  static constexpr int TEAMS = W == 1 ? LN_WAVES : 1;
+};
+
+// A parameter of either type; a null one is `one`.
+__device__ __forceinline__ float ln_param(const void* p, int dt, int64_t col, float none) {
+  if (!p) return none;
+  return dt == DT_BF16 ? bf16_to_f32(((const uint16_t*)p)[col]) : ((const float*)p)[col];
+}
+
+template <int DT, int W, int NV>
+__global__ __launch_bounds__(LnTeam<W>::THREADS) void ln_forward_kernel(LnForwardArgs a) {
+  __shared__ float red[2 * W];
+  constexpr int LANES = W * WAVE;
+  const int lane = (int)threadIdx.x % LANES, team = (int)threadIdx.x / LANES;
+  const int d = a.d;
+  const float inv_d = 1.f / (float)d;
+  float gain[NV][8], bias[NV][8];
+#pragma unroll
+  for (int j = 0; j < NV; ++j)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const int col = (lane + j * LANES) * 8 + e;
+      gain[j][e] = col < d ? ln_param(a.gain, a.param_dt, col, 1.f) : 0.f;
+      bias[j][e] = col < d ? ln_param(a.bias, a.param_dt, col, 0.f) : 0.f;
+    }
+  for (int64_t row = (int64_t)blockIdx.x * LnTeam<W>::TEAMS + team; row < a.rows;
+       row += (int64_t)gridDim.x * LnTeam<W>::TEAMS) {
+    const char* x = (const char*)a.x + row * a.ldx * Oct<DT>::ES;
+    char* y = (char*)a.y + row * a.ldy * Oct<DT>::ES;
+    Oct<DT> v[NV];
+    float sum = 0.f, none = 0.f;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      const int col = (lane + j * LANES) * 8;
+      v[j].load(x + (int64_t)col * Oct<DT>::ES, d - col);
+    }
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) sum += v[j].at(e);
+    team_sum2<W>(sum, none, red);
+    const float about = sum * inv_d;
+    float sq = 0.f, rest = 0.f;
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float c = v[j].at(e) - about;
+        if ((lane + j * LANES) * 8 + e < d) {
+          sq = fmaf(c, c, sq);
+          rest += c;
+        }
+      }
+    team_sum2<W>(sq, rest, red);
+    // The first mean is off by its roundings; the differences tell by how much.
+    rest *= inv_d;
+    const float mean = about + rest;
+    const float var = fmaxf(fmaf(-rest, rest, sq * inv_d), 0.f);
+    const float rstd = 1.f / sqrtf((sq != sq ? sq : var) + a.eps);
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      const int col = (lane + j * LANES) * 8;
+      float o[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) o[e] = fmaf((v[j].at(e) - mean) * rstd, gain[j][e], bias[j][e]);
+      v[j].set(o);
+      v[j].store(y + (int64_t)col * Oct<DT>::ES, d - col);
+    }
+    if (lane == 0) {
+      if (a.mean) a.mean[row] = mean;
+      if (a.rstd) a.rstd[row] = rstd;
+    }
+  }
+}
+
+// Item: (example b, range s of a.span rows). DX: dx is wanted; WG: the gradients are.
+template <int DT, int W, int NV, bool DX, bool WG>
+__global__ __launch_bounds__(LnTeam<W>::THREADS) void ln_backward_kernel(LnBackwardArgs a) {
+  constexpr int LANES = W * WAVE, TEAMS = LnTeam<W>::TEAMS;
+  __shared__ float red[2 * W];
+  __shared__ float meet[WG && TEAMS > 1 ? TEAMS : 1][WG && TEAMS > 1 ? 2 * 8 * WAVE : 1];
+  __shared__ float sq_red[LnTeam<W>::THREADS / WAVE];
+  const int lane = (int)threadIdx.x % LANES, team = (int)threadIdx.x / LANES;
+  const uint32_t item = xcd_remap(blockIdx.x, gridDim.x);
+  const int b = (int)(item / (uint32_t)a.ranges), s = (int)(item - (uint32_t)b * a.ranges);
+  const int d = a.d;
+  const float inv_d = 1.f / (float)d;
+  const int t0 = s * a.span, t1 = min(t0 + a.span, a.T);
+  float gain[NV][8];
+  float dg[NV][8], db[NV][8];
+#pragma unroll
+  for (int j = 0; j < NV; ++j)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const int col = (lane + j * LANES) * 8 + e;
+      gain[j][e] = DX && col < d ? ln_param(a.gain, a.param_dt, col, 1.f) : 0.f;
+      dg[j][e] = db[j][e] = 0.f;
+    }
+  for (int t = t0 + team; t < t1; t += TEAMS) {
+    const int64_t row = (int64_t)b * a.T + t;
+    const char* px = (const char*)a.x + row * a.ldx * Oct<DT>::ES;
+    const char* pg = (const char*)a.gy + row * a.ldgy * Oct<DT>::ES;
+    Oct<DT> x[NV], g[NV];
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      const int col = (lane + j * LANES) * 8;
+      x[j].load(px + (int64_t)col * Oct<DT>::ES, d - col);
+      g[j].load(pg + (int64_t)col * Oct<DT>::ES, d - col);
+    }
+    const float mean = a.mean[row], rstd = a.rstd[row];
+    float s1 = 0.f, s2 = 0.f;
+    // Features past d have gy = 0 here, so their xhat drops out of every sum.
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float gy = g[j].at(e), xh = (x[j].at(e) - mean) * rstd;
+        if constexpr (WG) {
+          dg[j][e] = fmaf(gy, xh, dg[j][e]);
+          db[j][e] += gy;
+        }
+        if constexpr (DX) {
+          const float w = gy * gain[j][e];
+          s1 += w;
+          s2 = fmaf(w, xh, s2);
+        }
+      }
+    if constexpr (DX) {
+      team_sum2<W>(s1, s2, red);
+      const float c1 = s1 * inv_d, c2 = s2 * inv_d;
+      char* pd = (char*)a.dx + row * a.lddx * Oct<DT>::ES;
+#pragma unroll
+      for (int j = 0; j < NV; ++j) {
+        const int col = (lane + j * LANES) * 8;
+        float o[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float xh = (x[j].at(e) - mean) * rstd;
+          o[e] = rstd * (g[j].at(e) * gain[j][e] - c1 - xh * c2);
+        }
+        if (a.accumulate_dx) {
+          Oct<DT> p;
+          p.load(pd + (int64_t)col * Oct<DT>::ES, d - col);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) o[e] += p.at(e);
+        }
+        x[j].set(o);
+        x[j].store(pd + (int64_t)col * Oct<DT>::ES, d - col);
+      }
+    }
+  }
+  if constexpr (WG) {
+    // The teams' sums meet in LDS, one octet of every lane at a time.
+    float* part = a.ranges > 1 ? a.ws + ((int64_t)b * a.ranges + s) * 2 * d : nullptr;
+    float* out_g = part ? part : a.dgain ? a.dgain + (int64_t)b * d : nullptr;
+    float* out_b = part ? part + d : a.dbias ? a.dbias + (int64_t)b * d : nullptr;
+    float sq = 0.f;
+    auto put = [&](int col, float vg, float vb) {
+      if (col >= d) return;
+      if (out_g) out_g[col] = vg;
+      if (out_b) out_b[col] = vb;
+      if (a.dgain) sq = fmaf(vg, vg, sq);
+      if (a.dbias) sq = fmaf(vb, vb, sq);
+    };
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      if constexpr (TEAMS > 1) {
+        __syncthreads();
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          meet[team][e * WAVE + lane] = dg[j][e];
+          meet[team][(8 + e) * WAVE + lane] = db[j][e];
+        }
+        __syncthreads();
+        const int e = team;   // TEAMS == 8: a team takes one element of every octet
+        float vg = 0.f, vb = 0.f;
+#pragma unroll
+        for (int w = 0; w < TEAMS; ++w) {
+          vg += meet[w][e * WAVE + lane];
+          vb += meet[w][(8 + e) * WAVE + lane];
+        }
+        put((lane + j * LANES) * 8 + e, vg, vb);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) put((lane + j * LANES) * 8 + e, dg[j][e], db[j][e]);
+      }
+    }
+    if (a.ranges == 1 && a.norm2) {
+      sq = wave_sum(sq);
+      if (threadIdx.x % WAVE == 0) sq_red[threadIdx.x / WAVE] = sq;
+      __syncthreads();
+      if (threadIdx.x == 0) {
+        float v = 0.f;
+        for (int w = 0; w < LnTeam<W>::THREADS / WAVE; ++w) v += sq_red[w];
+        a.norm2[b] = (a.accumulate ? a.norm2[b] : 0.f) + v;
+      }
+    }
+  }
+}
+static_assert(LN_WAVES == 8, "a team per element of an octet");
+
+// The ranges' partial sums of example blockIdx.y, 64 features at a time by
+// 4 groups of threads that each add every fourth range (then the groups, in
+// order). One workgroup per example writes the norm itself; several leave
+// a partial each.
+__global__ __launch_bounds__(256) void ln_finish_kernel(LnBackwardArgs a) {
+  __shared__ float meet[4][2][64];
+  __shared__ float sq_red[4];
+  const int b = (int)blockIdx.y, c = (int)threadIdx.x % 64, grp = (int)threadIdx.x / 64;
+  const int d = a.d;
+  const float* ws = a.ws + (int64_t)b * a.ranges * 2 * d;
+  float sq = 0.f;
+  for (int c0 = (int)blockIdx.x * 64; c0 < d; c0 += (int)gridDim.x * 64) {
+    const int col = c0 + c;
+    float vg = 0.f, vb = 0.f;
+    if (col < d) {
+#pragma unroll 4
+      for (int s = grp; s < a.ranges; s += 4) {
+        vg += ws[(int64_t)s * 2 * d + col];
+        vb += ws[(int64_t)s * 2 * d + d + col];
+      }
+    }
+    __syncthreads();
+    meet[grp][0][c] = vg;
+    meet[grp][1][c] = vb;
+    __syncthreads();
+    if (grp == 0 && col < d) {
+      vg = meet[0][0][c] + meet[1][0][c] + meet[2][0][c] + meet[3][0][c];
+      vb = meet[0][1][c] + meet[1][1][c] + meet[2][1][c] + meet[3][1][c];
+      if (a.dgain) { a.dgain[(int64_t)b * d + col] = vg; sq = fmaf(vg, vg, sq); }
+      if (a.dbias) { a.dbias[(int64_t)b * d + col] = vb; sq = fmaf(vb, vb, sq); }
+    }
+  }
+  if (!a.norm2) return;
+  sq = wave_sum(sq);   // only the first wave holds any
+  (void)sq_red;
+  if (threadIdx.x == 0) {
+    if (gridDim.x == 1)
+      a.norm2[b] = (a.accumulate ? a.norm2[b] : 0.f) + sq;
+    else
+      a.sq[(int64_t)b * gridDim.x + blockIdx.x] = sq;
+  }
+}
+
+template <int DT, int W, int NV>
+static hipError_t ln_forward(const LnForwardArgs& a, hipStream_t s) {
+  const int64_t need = (a.rows + LnTeam<W>::TEAMS - 1) / LnTeam<W>::TEAMS;
+  const unsigned grid = (unsigned)(need < 2048 ? need : 2048);
+  hipLaunchKernelGGL((ln_forward_kernel<DT, W, NV>), dim3(grid), dim3(LnTeam<W>::THREADS), 0, s, a);
+  return hipGetLastError();
+}
+
+template <int DT, int W, int NV>
+static hipError_t ln_backward(const LnBackwardArgs& a, hipStream_t s) {
+  const dim3 grid((unsigned)((int64_t)a.B * a.ranges)), block(LnTeam<W>::THREADS);
+  const bool wg = a.dgain || a.dbias;
+  if (a.dx && wg)
+    hipLaunchKernelGGL((ln_backward_kernel<DT, W, NV, true, true>), grid, block, 0, s, a);
+  else if (a.dx)
+    hipLaunchKernelGGL((ln_backward_kernel<DT, W, NV, true, false>), grid, block, 0, s, a);
+  else
+    hipLaunchKernelGGL((ln_backward_kernel<DT, W, NV, false, true>), grid, block, 0, s, a);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || a.ranges == 1 || !wg) return e;
+  hipLaunchKernelGGL(ln_finish_kernel, dim3((unsigned)a.chunks, (unsigned)a.B), dim3(256), 0, s, a);
+  e = hipGetLastError();
+  if (e != hipSuccess || !a.norm2 || a.chunks == 1) return e;
+  return launch_finish_rows(a.sq, a.B, a.chunks, a.norm2, a.accumulate, 1.f, s);
+}
+
+// Calls f<W, NV> for the team that holds rows of d features.
+#define DPG_LN_TEAMS(FN, DT)                       \
+  do {                                             \
+    const int octs = (a.d + 7) / 8;                \
+    if (octs <= 64) return FN<DT, 1, 1>(a, s);     \
+    if (octs <= 128) return FN<DT, 1, 2>(a, s);    \
+    if (octs <= 256) return FN<DT, 1, 4>(a, s);    \
+    if (octs <= 512) return FN<DT, 4, 2>(a, s);    \
+    if (octs <= 1024) return FN<DT, 4, 4>(a, s);   \
+    if (octs <= 2048) return FN<DT, 16, 2>(a, s);  \
+    return FN<DT, 16, 4>(a, s);                    \
+  } while (0)
+
+hipError_t launch_ln_forward(const LnForwardArgs& a, int dt, hipStream_t s) {
+  if (dt == DT_BF16) DPG_LN_TEAMS(ln_forward, DT_BF16);
+  DPG_LN_TEAMS(ln_forward, DT_F32);
+}
+
+hipError_t launch_ln_backward(const LnBackwardArgs& a, int dt, hipStream_t s) {
+  if (dt == DT_BF16) DPG_LN_TEAMS(ln_backward, DT_BF16);
+  DPG_LN_TEAMS(ln_backward, DT_F32);
+}
+#undef DPG_LN_TEAMS
+
+}  // namespace dpg

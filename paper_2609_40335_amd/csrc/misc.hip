@@ -1,6 +1,7 @@
 // Clip factors (eq. 2, eq. 7) and the Gaussian noise of eq. 3.
 #include "common.hpp"
 #include "kernels.hpp"
+#include "loss.hpp"
 
 namespace dpg {
 

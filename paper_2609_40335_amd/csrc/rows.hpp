@@ -1,0 +1,107 @@
+// Octets (8 consecutive elements) of rows of any alignment, and sums over the
+// threads that share a row. A part of the sources that include it.
+#pragma once
+#include "common.hpp"
+
+namespace dpg {
+
+constexpr float LOG2E = 1.4426950408889634f;
+
+typedef __attribute__((address_space(1))) u32x4_any global_u32x4_any_w;
+__device__ __forceinline__ void store16_any(char* p, const u32x4& v) {
+  *(global_u32x4_any_w*)(uintptr_t)p = v;
+}
+
+// An octet's bits as loaded: 16 bytes of bf16, 32 of fp32.
+template <int DT>
+struct Oct {
+  static constexpr int ES = DT == DT_BF16 ? 2 : 4;
+  u32x4 r[DT == DT_BF16 ? 1 : 2];
+
+  // Elements [0, n) at p (n may be past 8, or not positive: nothing is read); the
+  // others are `fill`, as bits of the type twice in a dword (bf16) or once (fp32).
+  __device__ __forceinline__ void load(const char* p, int64_t n, uint32_t fill = 0u) {
+    if (n >= 8) {
+      r[0] = load16_any(p);
+      if constexpr (DT == DT_F32) r[1] = load16_any(p + 16);
+      return;
+    }
+    if constexpr (DT == DT_BF16) {
+      r[0] = u32x4{fill, fill, fill, fill};
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (e < n) {
+          const uint32_t v = ((global_u16*)(uintptr_t)p)[e];
+          r[0][e >> 1] = (e & 1) ? (r[0][e >> 1] & 0xFFFFu) | (v << 16) : (r[0][e >> 1] & 0xFFFF0000u) | v;
+        }
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) r[e >> 2][e & 3] = e < n ? ((const uint32_t*)p)[e] : fill;
+    }
+  }
+
+  __device__ __forceinline__ float at(int e) const {
+    if constexpr (DT == DT_BF16)
+      return __uint_as_float((e & 1) ? r[0][e >> 1] & 0xFFFF0000u : r[0][e >> 1] << 16);
+    else
+      return __uint_as_float(r[e >> 2][e & 3]);
+  }
+
+  // Rounds eight values to the type (to nearest even; NaN stays NaN).
+  __device__ __forceinline__ void set(const float (&v)[8]) {
+    if constexpr (DT == DT_BF16) {
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        r[0][q] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{v[2 * q], v[2 * q + 1]}, bf16x2));
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) r[e >> 2][e & 3] = __float_as_uint(v[e]);
+    }
+  }
+
+  __device__ __forceinline__ void store(char* p, int64_t n) const {
+    if (n >= 8) {
+      store16_any(p, r[0]);
+      if constexpr (DT == DT_F32) store16_any(p + 16, r[1]);
+      return;
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (e < n) {
+        if constexpr (DT == DT_BF16)
+          ((uint16_t*)p)[e] = (uint16_t)(r[0][e >> 1] >> ((e & 1) * 16));
+        else
+          ((uint32_t*)p)[e] = r[e >> 2][e & 3];
+      }
+  }
+};
+
+// Sums of two values over a team of W waves, in every thread: W = 1 a wave of
+// its own, otherwise the whole workgroup through `red` (2 W floats), in a fixed order.
+template <int W>
+__device__ __forceinline__ void team_sum2(float& a, float& b, float* red) {
+#pragma unroll
+  for (int off = 8; off >= 1; off >>= 1) {
+    a += __shfl_xor(a, off, WAVE);
+    b += __shfl_xor(b, off, WAVE);
+  }
+  a = xor32_sum(xor16_sum(a));
+  b = xor32_sum(xor16_sum(b));
+  if constexpr (W > 1) {
+    const int w = (int)threadIdx.x / WAVE;
+    __syncthreads();   // the previous sums have been read
+    if (threadIdx.x % WAVE == 0) {
+      red[2 * w] = a;
+      red[2 * w + 1] = b;
+    }
+    __syncthreads();
+    a = b = 0.f;
+#pragma unroll
+    for (int i = 0; i < W; ++i) {
+      a += red[2 * i];
+      b += red[2 * i + 1];
+    }
+  }
+}
+
+}  // namespace dpg

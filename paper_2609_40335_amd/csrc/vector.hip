@@ -25,6 +25,7 @@
 // order, with the Gaussian mechanism of eq. 3 fused into the store.
 #include "common.hpp"
 #include "kernels.hpp"
+#include "layernorm.hpp"
 
 namespace dpg {
 

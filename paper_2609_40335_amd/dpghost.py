@@ -27,6 +27,8 @@ __all__ = [
     "dp_noise_fill", "dp_vector_grads_grouped", "dp_vector_clipped_sum_noised_grouped",
     "dp_ghost_norm_linear_bias_grouped", "VectorSums",
     "dp_ghost_norm_positional", "dp_clipped_grad_sum_positional_noised",
+    "dp_layernorm_forward", "dp_layernorm_backward",
+    "dp_token_logprobs", "dp_cross_entropy", "dp_preference_loss",
     "LinearGroup", "VectorGroup",
 ]
 
@@ -127,6 +129,16 @@ _SIGS = {
     "dp_ghost_norm_positional": ([_VP, _I64, _I, _I, _I, _I, _VP, _I, _VP, _SZ, _VP], _I),
     "dp_clipped_grad_sum_positional_noised": ([_VP, _I64, _VP, _I, _I, _I, _I, _VP, _I, _I64,
                                                _U64, _I, _F, _F, _I, _U64, _U64, _VP], _I),
+    "dp_layernorm_forward": ([_VP, _I64, _VP, _VP, _I, _I, _I, _I, _I, _F, _VP, _I64, _VP, _VP,
+                              _VP], _I),
+    "dp_layernorm_backward_workspace": ([_I, _I, _I], _SZ),
+    "dp_layernorm_backward": ([_VP, _I64, _VP, _I64, _VP, _I, _VP, _VP, _I, _I, _I, _I, _VP, _I64,
+                               _I, _VP, _VP, _VP, _I, _VP, _SZ, _VP], _I),
+    "dp_token_logprobs": ([_VP, _I64, _VP, _I, _I, _I, _I, _VP, _VP, _VP], _I),
+    "dp_cross_entropy": ([_VP, _I64, _VP, _VP, _I, _I, _I, _I, _VP, _VP, _I64, _VP], _I),
+    "dp_preference_loss_workspace": ([_I, _I], _SZ),
+    "dp_preference_loss": ([_VP, _I64, _VP, _I, _VP, _F, _F, _I, _I, _I, _I, _VP, _VP, _VP, _VP,
+                            _I64, _VP, _SZ, _VP], _I),
 }
 
 
@@ -724,6 +736,146 @@ def dp_clipped_grad_sum_noised_store(layers: Sequence, outs: Sequence[torch.Tens
                                                   store.numel() * store.element_size(),
                                                   _stream(stream)),
            "dp_clipped_grad_sum_noised_store")
+
+
+
+def _same_device(stream, *named) -> None:
+    """Operands of one call: device tensors, all on the device the call is made on
+    (the stream's, or the current one)."""
+    at = torch.cuda.current_device() if stream is None else getattr(stream, "device_index",
+                                                                   torch.cuda.current_device())
+    if at != torch.cuda.current_device():
+        raise DPError("the stream belongs to another device than the current one")
+    for t, name in named:
+        if t is None:
+            continue
+        _dev(t, name)
+        if t.device.index != at:
+            raise DPError(f"{name} is on {t.device}, the call on cuda:{at}")
+
+
+def _f32(t, shape, name: str):
+    """Pointer of a contiguous fp32 tensor of this shape (None: NULL)."""
+    if t is None:
+        return None
+    if t.dtype != torch.float32 or tuple(t.shape) != shape or not t.is_contiguous():
+        raise DPError(f"{name} must be contiguous fp32 {list(shape)}")
+    return t.data_ptr()
+
+
+def _like(t, x, name: str, of: str):
+    """(pointer, row stride) of a tensor with x's shape and dtype."""
+    if t.dtype != x.dtype or t.shape != x.shape:
+        raise DPError(f"{name} must have {of}'s shape and dtype")
+    p, _, _, _, ld = _rows(t, name)
+    return p, ld
+
+
+def _params(d: int, **named):
+    """Pointers and the common dtype of parameters of d elements (None: NULL)."""
+    dt, ptrs = DP_F32, []
+    given = [t for t in named.values() if t is not None]
+    for name, t in named.items():
+        if t is None:
+            ptrs.append(None)
+            continue
+        if tuple(t.shape) != (d,) or not t.is_contiguous() or t.dtype != given[0].dtype:
+            raise DPError(f"{name} must be contiguous [{d}], gain and bias of one dtype")
+        dt = _dtype(t)
+        ptrs.append(t.data_ptr())
+    return ptrs, dt
+
+
+def dp_layernorm_forward(x, gain, bias, y, mean=None, rstd=None, eps: float = 1e-5,
+                         stream=None) -> torch.Tensor:
+    """y = gain * (x - mean) * rstd + bias per row of x [B, T, d]; gain, bias [d]
+    (fp32 or bf16, or None); mean and rstd: fp32 [B, T] outputs for the backward pass."""
+    _same_device(stream, (x, "x"), (gain, "gain"), (bias, "bias"), (y, "y"), (mean, "mean"),
+                 (rstd, "rstd"))
+    px, B, T, d, ldx = _rows(x, "x")
+    py, ldy = _like(y, x, "y", "x")
+    (pg, pb), pdt = _params(d, gain=gain, bias=bias)
+    _check(lib().dp_layernorm_forward(px, ldx, pg, pb, pdt, B, T, d, _dtype(x), float(eps), py,
+                                      ldy, _f32(mean, (B, T), "mean"), _f32(rstd, (B, T), "rstd"),
+                                      _stream(stream)), "dp_layernorm_forward")
+    return y
+
+
+def dp_layernorm_backward(gy, x, gain, mean, rstd, dx, dgain=None, dbias=None, norm2=None,
+                          accumulate: bool = False, accumulate_dx: bool = False,
+                          stream=None) -> None:
+    """From gy = d loss / d y: dx [B, T, d] (or None), the per-example gradients dgain
+    and dbias (fp32 [B, d], either may be None), and their squared norms into (accumulate:
+    added to) norm2 (fp32 [B] or None). accumulate_dx adds onto dx."""
+    L = lib()
+    _same_device(stream, (gy, "gy"), (x, "x"), (gain, "gain"), (mean, "mean"), (rstd, "rstd"),
+                 (dx, "dx"), (dgain, "dgain"), (dbias, "dbias"), (norm2, "norm2"))
+    pg, B, T, d, ldg = _rows(gy, "gy")
+    px, ldx = _like(x, gy, "x", "gy")
+    pd, ldd = (None, 0) if dx is None else _like(dx, gy, "dx", "gy")
+    (pw,), pdt = _params(d, gain=gain)
+    ws, nbytes = None, 0
+    if dgain is not None or dbias is not None:
+        nbytes = L.dp_layernorm_backward_workspace(B, T, d)
+        ws = _ws(nbytes, gy.device, stream) if nbytes else None
+    _check(L.dp_layernorm_backward(pg, ldg, px, ldx, pw, pdt, _f32(mean, (B, T), "mean"),
+                                   _f32(rstd, (B, T), "rstd"), B, T, d, _dtype(gy), pd, ldd,
+                                   int(accumulate_dx), _f32(dgain, (B, d), "dgain"),
+                                   _f32(dbias, (B, d), "dbias"), _f32(norm2, (B,), "norm2"),
+                                   int(accumulate), None if ws is None else ws.data_ptr(), nbytes,
+                                   _stream(stream)), "dp_layernorm_backward")
+
+
+def _logits(Z, targets):
+    pz, B, T, V, ldz = _rows(Z, "Z")
+    if targets.dtype != torch.int32 or tuple(targets.shape) != (B, T) or not targets.is_contiguous():
+        raise DPError("targets must be contiguous int32 [B, T]")
+    return pz, B, T, V, ldz
+
+
+def dp_token_logprobs(Z, targets, logp, lse=None, stream=None) -> torch.Tensor:
+    """logp [B, T] = log softmax(Z)[target] (0 where the target is outside [0, V)),
+    lse [B, T] the logarithm of the row's sum of exponentials."""
+    _same_device(stream, (Z, "Z"), (targets, "targets"), (logp, "logp"), (lse, "lse"))
+    pz, B, T, V, ldz = _logits(Z, targets)
+    _check(lib().dp_token_logprobs(pz, ldz, targets.data_ptr(), B, T, V, _dtype(Z),
+                                   _f32(logp, (B, T), "logp"), _f32(lse, (B, T), "lse"),
+                                   _stream(stream)), "dp_token_logprobs")
+    return logp
+
+
+def dp_cross_entropy(Z, targets, w, logp, Gz, stream=None) -> torch.Tensor:
+    """Gz = w (softmax(Z) - onehot(targets)), the gradient of sum_t w (-logp); logp
+    (fp32 [B, T] or None) as dp_token_logprobs. Gz may be Z."""
+    _same_device(stream, (Z, "Z"), (targets, "targets"), (w, "w"), (logp, "logp"), (Gz, "Gz"))
+    pz, B, T, V, ldz = _logits(Z, targets)
+    pg, ldg = _like(Gz, Z, "Gz", "Z")
+    _check(lib().dp_cross_entropy(pz, ldz, targets.data_ptr(), _f32(w, (B, T), "w"), B, T, V,
+                                  _dtype(Z), _f32(logp, (B, T), "logp"), pg, ldg,
+                                  _stream(stream)), "dp_cross_entropy")
+    return Gz
+
+
+def dp_preference_loss(Z, targets, split: int, ref_logp, beta: float, loss, rewards=None,
+                       logp=None, Gz=None, label_smoothing: float = 0.0,
+                       stream=None) -> torch.Tensor:
+    """Loss [B] of pairs of answers (tokens before split: the chosen one) against a
+    reference model's log-probabilities ref_logp [B, T] (or None); rewards [B, 2], logp
+    [B, T] and Gz = d loss / d Z are optional. Gz may be Z."""
+    L = lib()
+    _same_device(stream, (Z, "Z"), (targets, "targets"), (ref_logp, "ref_logp"), (loss, "loss"),
+                 (rewards, "rewards"), (logp, "logp"), (Gz, "Gz"))
+    pz, B, T, V, ldz = _logits(Z, targets)
+    pg, ldg = (None, 0) if Gz is None else _like(Gz, Z, "Gz", "Z")
+    nbytes = L.dp_preference_loss_workspace(B, T)
+    ws = _ws(nbytes, Z.device, stream)
+    _check(L.dp_preference_loss(pz, ldz, targets.data_ptr(), int(split),
+                                _f32(ref_logp, (B, T), "ref_logp"), float(beta),
+                                float(label_smoothing), B, T, V, _dtype(Z),
+                                _f32(loss, (B,), "loss"), _f32(rewards, (B, 2), "rewards"),
+                                _f32(logp, (B, T), "logp"), pg, ldg, ws.data_ptr(), nbytes,
+                                _stream(stream)), "dp_preference_loss")
+    return loss
 
 
 class LinearGroup:
