@@ -588,6 +588,41 @@ dp_status_t dp_preference_loss(const void* Z, int64_t ldz, const int32_t* target
                                float* logp, void* Gz, int64_t ldg, void* workspace,
                                size_t workspace_bytes, void* stream);
 
+/* ---------------------------------------------------------------------
+ * Orthogonalised updates: Newton-Schulz products that drive the singular
+ * values of a noised sum (or of a momentum of them) towards 1, as the Muon
+ * optimiser does with a weight matrix's momentum. With X_0 = G/(||G||_F + eps),
+ *   X <- a_k X + b_k (X X^T) X + c_k (X X^T)^2 X      for k = 0 .. steps-1
+ *   out = (accumulate ? out : 0) + scale * X_steps
+ * for every matrix of the group: G [rows, cols] (in_dt, row stride ldg), out
+ * [rows, cols] (out_dt, row stride ldo; may be G with its row stride and type).
+ * coef is a host array of steps * 3 floats (a_k, b_k, c_k); eps >= 0 keeps a
+ * zero matrix zero. With accumulate, scale = -(learning rate) updates a weight
+ * matrix in place. NaN or inf in G makes that matrix's update NaN.
+ * out_dt also chooses the products' precision: DP_F32 comes within about 1e-6
+ * of exact arithmetic; DP_BF16 rounds operands to 11 bits, of the order of the result's own
+ * rounding for sums under noise (1e-3 to 2e-3 of the result; more
+ * where a few directions outweigh all others: 7e-3 at 30 times their norm).
+ * Singular values must stay below 8 between steps, as they do for the usual
+ * coefficients (3.4445, -4.7750, 2.0315; or 15/8, -10/8, 3/8).
+ * Sides up to 65536 (else DP_EUNSUPPORTED), 1 <= steps <= 64. The workspace
+ * is dp_orthogonalize_workspace() bytes (about 12 bytes an element of G for
+ * DP_F32, 6 for DP_BF16, and 4 or 8 m^2 more for a shorter side m), 16-byte aligned.
+ * ------------------------------------------------------------------- */
+typedef struct {
+  const void* G;
+  int64_t ldg;
+  void* out;
+  int64_t ldo;
+  int32_t rows, cols;
+  float scale;
+} dp_matrix_t;
+size_t dp_orthogonalize_workspace(const dp_matrix_t* matrices, int n, dp_dtype_t out_dt);
+dp_status_t dp_orthogonalize_grouped(const dp_matrix_t* matrices, int n, dp_dtype_t in_dt,
+                                     dp_dtype_t out_dt, const float* coef, int steps, float eps,
+                                     int accumulate, void* workspace, size_t workspace_bytes,
+                                     void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -22,7 +22,7 @@ BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libdpghost.so")
 SOURCES = ["gram.hip", "gemm.hip", "embed.hip", "misc.hip", "vector.hip", "api.cpp"]
 HEADERS = ["common.hpp", "kernels.hpp", "rows.hpp", "layernorm.hpp", "loss.hpp",
-           "api_step.hpp"]
+           "orthogonalize.hpp", "api_step.hpp"]
 
 ARCH = "gfx950"
 DEVICE_FLAGS = ["-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]

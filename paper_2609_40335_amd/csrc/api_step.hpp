@@ -59,6 +59,29 @@ dp_status_t check_in_place(const void* Z, int64_t ldz, const void* Gz, int64_t l
   return DP_OK;
 }
 
+inline int ns_padded(int x) { return (int)ceil_div(x, dpg::NS_TILE) * dpg::NS_TILE; }
+inline int ns_planes(dp_dtype_t out_dt) { return out_dt == DP_BF16 ? 1 : 2; }
+
+// Checks the sizes and strides; *bytes gets the workspace the group needs.
+dp_status_t check_matrices(const dp_matrix_t* m, int n, dp_dtype_t in_dt, dp_dtype_t out_dt,
+                           size_t* bytes) {
+  if (!m || n <= 0) return fail(DP_EINVAL, "no matrices");
+  if (!dtype_ok(in_dt)) return fail(DP_EINVAL, "unknown dtype %d", (int)in_dt);
+  if (!dtype_ok(out_dt)) return fail(DP_EINVAL, "unknown dtype %d", (int)out_dt);
+  *bytes = 0;
+  for (int l = 0; l < n; ++l) {
+    const dp_matrix_t& x = m[l];
+    if (x.rows <= 0 || x.cols <= 0) return fail(DP_EINVAL, "matrix %d: empty", l);
+    if (x.rows > dpg::NS_MAX_SIDE || x.cols > dpg::NS_MAX_SIDE)
+      return fail(DP_EUNSUPPORTED, "matrix %d: a side exceeds %d", l, dpg::NS_MAX_SIDE);
+    if (x.ldg < x.cols || x.ldo < x.cols)
+      return fail(DP_EINVAL, "matrix %d: row stride smaller than its columns", l);
+    *bytes += align_up(dpg::ns_bytes(ns_padded(std::min(x.rows, x.cols)),
+                                     ns_padded(std::max(x.rows, x.cols)), ns_planes(out_dt)));
+  }
+  return DP_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -204,6 +227,54 @@ dp_status_t dp_preference_loss(const void* Z, int64_t ldz, const int32_t* target
     if (st != DP_OK) return st;
     if (!Gz) continue;
     st = hip_status(dpg::launch_logit_grads(a, kdt(dt), s), "logit_grads launch");
+    if (st != DP_OK) return st;
+  }
+  return DP_OK;
+}
+
+size_t dp_orthogonalize_workspace(const dp_matrix_t* matrices, int n, dp_dtype_t out_dt) {
+  size_t bytes = 0;
+  return check_matrices(matrices, n, DP_F32, out_dt, &bytes) == DP_OK ? bytes : 0;
+}
+
+dp_status_t dp_orthogonalize_grouped(const dp_matrix_t* matrices, int n, dp_dtype_t in_dt,
+                                     dp_dtype_t out_dt, const float* coef, int steps, float eps,
+                                     int accumulate, void* workspace, size_t workspace_bytes,
+                                     void* stream) {
+  size_t need = 0;
+  dp_status_t st = check_matrices(matrices, n, in_dt, out_dt, &need);
+  if (st != DP_OK) return st;
+  if (!coef) return fail(DP_EINVAL, "coef is NULL");
+  if (steps < 1 || steps > dpg::NS_MAX_STEPS)
+    return fail(DP_EINVAL, "steps = %d is not in [1, %d]", steps, dpg::NS_MAX_STEPS);
+  for (int k = 0; k < 3 * steps; ++k)
+    if (!std::isfinite(coef[k])) return fail(DP_EINVAL, "coef[%d] is not finite", k);
+  if (!(eps >= 0.f) || !std::isfinite(eps)) return fail(DP_EINVAL, "eps must be >= 0");
+  for (int l = 0; l < n; ++l) {
+    if (!matrices[l].G || !matrices[l].out) return fail(DP_EINVAL, "matrix %d: G or out is NULL", l);
+    if (!std::isfinite(matrices[l].scale)) return fail(DP_EINVAL, "matrix %d: scale is not finite", l);
+  }
+  if (!workspace || workspace_bytes < need)
+    return fail(DP_EINVAL, "workspace of %zu bytes needed", need);
+  if (!aligned16(workspace)) return fail(DP_EINVAL, "workspace must be 16-byte aligned");
+  char* ws = static_cast<char*>(workspace);
+  for (int l0 = 0; l0 < n; l0 += dpg::NS_MAX_MATS) {
+    dpg::NsArgs a{};
+    a.n = std::min(n - l0, dpg::NS_MAX_MATS);
+    a.out_dt = kdt(out_dt); a.accumulate = accumulate ? 1 : 0; a.eps = eps;
+    for (int l = 0; l < a.n; ++l) {
+      const dp_matrix_t& x = matrices[l0 + l];
+      dpg::NsMat& M = a.M[l];
+      M.G = x.G; M.out = x.out; M.ldg = x.ldg; M.ldo = x.ldo;
+      M.rows = x.rows; M.cols = x.cols; M.scale = x.scale;
+      M.mp = ns_padded(std::min(x.rows, x.cols));
+      M.np = ns_padded(std::max(x.rows, x.cols));
+      M.ws = ws;
+      ws += align_up(dpg::ns_bytes(M.mp, M.np, ns_planes(out_dt)));
+    }
+    st = hip_status(dpg::launch_orthogonalize(a, kdt(in_dt), ns_planes(out_dt), coef, steps,
+                                              as_stream(stream)),
+                    "orthogonalize launch");
     if (st != DP_OK) return st;
   }
   return DP_OK;

@@ -518,6 +518,56 @@ inline int64_t preference_pairs(int B, int T, int V, int es) {
 }
 hipError_t launch_preference(const PreferenceArgs& a, int B, hipStream_t s);
 
+// ---------------------------------------------------- orthogonalised updates
+constexpr int NS_TILE = 128;        // rows and columns of an output tile; sizes are padded to it
+constexpr int NS_MAX_MATS = 56;     // matrices per launch (kernel arguments stay < 4 KiB)
+constexpr int NS_MAX_SIDE = 65536;
+constexpr int NS_MAX_STEPS = 64;
+enum { NS_GRAM = 0, NS_POLY = 1, NS_UPDATE = 2 };                    // the three products of a step
+enum { NS_X = 0, NS_XT0 = 1, NS_XT1 = 2, NS_A = 3, NS_P = 4 };       // a matrix's buffers
+
+struct NsMat {
+  const void* G;        // [rows, ldg]
+  void* out;            // [rows, ldo]
+  char* ws;             // partial sums of squares, then the buffers
+  int64_t ldg, ldo;
+  int32_t rows, cols;
+  int32_t mp, np;       // shorter and longer side, padded
+  float scale;
+  uint32_t item_begin;  // first work item of this matrix in a launch
+};
+struct NsArgs {
+  NsMat M[NS_MAX_MATS];
+  int32_t n;
+  int32_t out_dt, accumulate;
+  int32_t step, last;
+  float coef[3];
+  float eps;
+};
+static_assert(sizeof(NsArgs) <= 4096, "kernel arguments must stay within 4 KiB");
+static_assert(NS_MAX_MATS <= 64, "a wave finds a work item's matrix with one lane per entry");
+
+constexpr int NS_PARTS = 128;       // most partial sums of squares of a matrix
+constexpr size_t NS_HEAD = NS_PARTS * 8;
+#define DPG_HD __host__ __device__
+// Workgroups that sum a matrix's squares: 32768 elements each, or NS_PARTS of them.
+DPG_HD inline int ns_parts(int rows, int cols) {
+  const int64_t p = ((int64_t)rows * cols + 32767) / 32768;
+  return p < 1 ? 1 : p > NS_PARTS ? NS_PARTS : (int)p;
+}
+// Offset of plane `plane` (of pl) of buffer `which`: X [mp, np], X^T [np, mp] twice, A and P [mp, mp].
+DPG_HD inline size_t ns_offset(int mp, int np, int which, int plane, int pl) {
+  const size_t x = (size_t)mp * np * 2, q = (size_t)mp * mp * 2;
+  const size_t at = which <= NS_A ? (size_t)which * pl * x : 3 * (size_t)pl * x + (size_t)pl * q;
+  return NS_HEAD + at + (size_t)plane * (which < NS_A ? x : q);
+}
+DPG_HD inline size_t ns_bytes(int mp, int np, int pl) {
+  return ns_offset(mp, np, NS_P, 0, pl) + (size_t)pl * mp * mp * 2;
+}
+#undef DPG_HD
+hipError_t launch_orthogonalize(const NsArgs& a, int dt, int planes, const float* coef, int steps,
+                                hipStream_t s);
+
 // ----------------------------------------------------------- clip and noise
 // c (nullable) = clip factors; cs (nullable) = scale * clip factors; the
 // squared norm is norm2 (+ norm2_b when not null).

@@ -2,6 +2,7 @@
 #include "common.hpp"
 #include "kernels.hpp"
 #include "loss.hpp"
+#include "orthogonalize.hpp"
 
 namespace dpg {
 

@@ -29,6 +29,7 @@ __all__ = [
     "dp_ghost_norm_positional", "dp_clipped_grad_sum_positional_noised",
     "dp_layernorm_forward", "dp_layernorm_backward",
     "dp_token_logprobs", "dp_cross_entropy", "dp_preference_loss",
+    "dp_orthogonalize_grouped", "NS_QUINTIC",
     "LinearGroup", "VectorGroup",
 ]
 
@@ -52,6 +53,12 @@ class dp_linear_t(ctypes.Structure):
 class dp_vector_t(ctypes.Structure):
     _fields_ = [("X", ctypes.c_void_p), ("ldx", ctypes.c_int64), ("G", ctypes.c_void_p),
                 ("ldg", ctypes.c_int64), ("d", ctypes.c_int32)]
+
+
+class dp_matrix_t(ctypes.Structure):
+    _fields_ = [("G", ctypes.c_void_p), ("ldg", ctypes.c_int64), ("out", ctypes.c_void_p),
+                ("ldo", ctypes.c_int64), ("rows", ctypes.c_int32), ("cols", ctypes.c_int32),
+                ("scale", ctypes.c_float)]
 
 
 def library_path() -> str:
@@ -136,6 +143,9 @@ _SIGS = {
                                _I, _VP, _VP, _VP, _I, _VP, _SZ, _VP], _I),
     "dp_token_logprobs": ([_VP, _I64, _VP, _I, _I, _I, _I, _VP, _VP, _VP], _I),
     "dp_cross_entropy": ([_VP, _I64, _VP, _VP, _I, _I, _I, _I, _VP, _VP, _I64, _VP], _I),
+    "dp_orthogonalize_workspace": ([ctypes.POINTER(dp_matrix_t), _I, _I], _SZ),
+    "dp_orthogonalize_grouped": ([ctypes.POINTER(dp_matrix_t), _I, _I, _I, ctypes.POINTER(_F), _I,
+                                  _F, _I, _VP, _SZ, _VP], _I),
     "dp_preference_loss_workspace": ([_I, _I], _SZ),
     "dp_preference_loss": ([_VP, _I64, _VP, _I, _VP, _F, _F, _I, _I, _I, _I, _VP, _VP, _VP, _VP,
                             _I64, _VP, _SZ, _VP], _I),
@@ -876,6 +886,50 @@ def dp_preference_loss(Z, targets, split: int, ref_logp, beta: float, loss, rewa
                                 _f32(logp, (B, T), "logp"), pg, ldg, ws.data_ptr(), nbytes,
                                 _stream(stream)), "dp_preference_loss")
     return loss
+
+
+
+# Newton-Schulz coefficients (a, b, c) that bring singular values near 1 in about five steps.
+NS_QUINTIC = (3.4445, -4.7750, 2.0315)
+
+
+def dp_orthogonalize_grouped(grads: Sequence[torch.Tensor], outs: Sequence[torch.Tensor],
+                             coef=NS_QUINTIC, steps: int = 5, scale=1.0, eps: float = 1e-7,
+                             accumulate: bool = False, stream=None) -> None:
+    """outs[l] (+)= scale * the Newton-Schulz orthogonalisation of grads[l], 2-D tensors with
+    unit column stride and one dtype per side (fp32 or bf16; the outputs' chooses the
+    precision). coef: (a, b, c), or one such triple per step; scale: a number or one per matrix."""
+    L = lib()
+    n = len(grads)
+    if n == 0 or len(outs) != n:
+        raise DPError("one output per matrix, at least one")
+    scales = list(scale) if isinstance(scale, (list, tuple)) else [scale] * n
+    if len(scales) != n:
+        raise DPError("one scale per matrix")
+    _same_device(stream, *((g, f"grads[{l}]") for l, g in enumerate(grads)),
+                 *((o, f"outs[{l}]") for l, o in enumerate(outs)))
+    dt, odt = grads[0].dtype, outs[0].dtype
+    arr = (dp_matrix_t * n)()
+    for l, (g, o) in enumerate(zip(grads, outs)):
+        if g.dim() != 2 or g.shape != o.shape or g.dtype != dt or o.dtype != odt:
+            raise DPError("grads and outs are 2-D, of the same shapes, and of one dtype each")
+        r, c = g.shape
+        if (c > 1 and (g.stride(1) != 1 or o.stride(1) != 1)):
+            raise DPError("matrices must have unit column stride")
+        arr[l] = dp_matrix_t(g.data_ptr(), max(g.stride(0), c) if r == 1 else g.stride(0),
+                             o.data_ptr(), max(o.stride(0), c) if r == 1 else o.stride(0), r, c,
+                             float(scales[l]))
+    flat = [float(v) for v in coef] * steps if not isinstance(coef[0], (list, tuple)) else \
+        [float(v) for k in coef for v in k]
+    if len(flat) != 3 * steps:
+        raise DPError("coef is (a, b, c), or one such triple per step")
+    cf = (ctypes.c_float * max(len(flat), 1))(*flat)
+    _dt, _odt = _dtype(grads[0]), _dtype(outs[0])
+    nbytes = L.dp_orthogonalize_workspace(arr, n, _odt)
+    ws = _ws(nbytes, grads[0].device, stream)
+    _check(L.dp_orthogonalize_grouped(arr, n, _dt, _odt, cf, int(steps), float(eps),
+                                      int(accumulate), ws.data_ptr(), nbytes, _stream(stream)),
+           "dp_orthogonalize_grouped")
 
 
 class LinearGroup:

@@ -168,3 +168,49 @@ def test_layernorm_formula_against_autograd():
     np.testing.assert_allclose(back["dx"], x.grad.numpy(), rtol=1e-10, atol=1e-12)
     np.testing.assert_allclose(back["dgain"].sum(0), gain.grad.numpy(), rtol=1e-11)
     np.testing.assert_allclose(back["dbias"].sum(0), bias.grad.numpy(), rtol=1e-11)
+
+
+def _matrix(G=P[0], ldg=64, out=P[1], ldo=64, rows=32, cols=64, scale=1.0):
+    return D.dp_matrix_t(G, ldg, out, ldo, rows, cols, scale)
+
+
+def _orth(L, m=None, n=1, dt=0, odt=0, coef=(1.0, 2.0, 3.0), steps=1, eps=0.0, ws=P[2], nbytes=1 << 40):
+    import ctypes
+    arr = (D.dp_matrix_t * 1)(m if m is not None else _matrix())
+    cf = None if coef is None else (ctypes.c_float * len(coef))(*coef)
+    return L.dp_orthogonalize_grouped(arr, n, dt, odt, cf, steps, eps, 0, ws, nbytes, None)
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(n=0), EINVAL), (dict(dt=3), EINVAL), (dict(odt=3), EINVAL), (dict(coef=None), EINVAL),
+    (dict(coef=(1.0, float("nan"), 0.0)), EINVAL), (dict(steps=0), EINVAL),
+    (dict(steps=65, coef=(0.0,) * 195), EINVAL), (dict(eps=-1.0), EINVAL),
+    (dict(eps=float("inf")), EINVAL), (dict(ws=None), EINVAL), (dict(nbytes=64), EINVAL),
+    (dict(ws=P[2] + 2), EINVAL), (dict(m=_matrix(G=None)), EINVAL), (dict(m=_matrix(out=None)), EINVAL),
+    (dict(m=_matrix(ldg=63)), EINVAL), (dict(m=_matrix(ldo=63)), EINVAL),
+    (dict(m=_matrix(rows=0)), EINVAL), (dict(m=_matrix(cols=-1)), EINVAL),
+    (dict(m=_matrix(scale=float("nan"))), EINVAL), (dict(m=_matrix(rows=65537)), EUNSUP),
+    (dict(m=_matrix(cols=65537, ldg=65537, ldo=65537)), EUNSUP)])
+def test_orthogonalize_refuses(L, kw, status):
+    assert _orth(L, **kw) == status, L.dp_last_error()
+
+
+def test_orthogonalize_workspace(L):
+    one, tall = (D.dp_matrix_t * 1)(_matrix()), (D.dp_matrix_t * 1)(_matrix(rows=64, cols=32, ldg=32, ldo=32))
+    assert L.dp_orthogonalize_workspace(one, 1, D.DP_BF16) == L.dp_orthogonalize_workspace(tall, 1, D.DP_BF16)
+    assert L.dp_orthogonalize_workspace(one, 1, D.DP_F32) > L.dp_orthogonalize_workspace(one, 1, D.DP_BF16) > 0
+    assert L.dp_orthogonalize_workspace(None, 1, D.DP_F32) == 0
+    assert L.dp_orthogonalize_workspace(one, 0, D.DP_F32) == 0
+
+
+def test_newton_schulz_formula():
+    """Singular values follow the polynomial; singular vectors stay."""
+    from tests.step_formulas import newton_schulz
+    g = np.random.default_rng(5).standard_normal((9, 17))
+    u, s, v = np.linalg.svd(g, full_matrices=False)
+    for G, (uu, vv) in ((g, (u, v)), (g.T, (v.T, u.T))):
+        x = s / np.linalg.norm(g)
+        for a, b, c in ((3.0, -2.0, 0.5), (1.5, -0.5, 0.0)):
+            x = a * x + b * x ** 3 + c * x ** 5
+        np.testing.assert_allclose(newton_schulz(G, [(3.0, -2.0, 0.5), (1.5, -0.5, 0.0)], 0.0),
+                                   uu @ np.diag(x) @ vv, atol=1e-13)
