@@ -605,9 +605,12 @@ dp_status_t dp_preference_loss(const void* Z, int64_t ldz, const int32_t* target
  * where a few directions outweigh all others: 7e-3 at 30 times their norm).
  * Singular values must stay below 8 between steps, as they do for the usual
  * coefficients (3.4445, -4.7750, 2.0315; or 15/8, -10/8, 3/8).
- * Sides up to 65536 (else DP_EUNSUPPORTED), 1 <= steps <= 64. The workspace
- * is dp_orthogonalize_workspace() bytes (about 12 bytes an element of G for
- * DP_F32, 6 for DP_BF16, and 4 or 8 m^2 more for a shorter side m), 16-byte aligned.
+ * Sides up to 65536 and, padded to multiples of 128, fewer than 2^30 elements (else
+ * DP_EUNSUPPORTED), 1 <= steps <= 64. The workspace is dp_orthogonalize_workspace()
+ * bytes, 16-byte aligned: about 8 bytes an element of G for DP_F32 and 4 for
+ * DP_BF16, and 8 or 4 m^2 more for a shorter side m, for the 48 largest matrices; 0 where
+ * all matrices are small enough to be worked in LDS (about 64 x 376 for DP_F32, 128 x 224 or
+ * 64 x 512 for DP_BF16).
  * ------------------------------------------------------------------- */
 typedef struct {
   const void* G;

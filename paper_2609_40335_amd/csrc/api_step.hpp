@@ -62,13 +62,37 @@ dp_status_t check_in_place(const void* Z, int64_t ldz, const void* Gz, int64_t l
 inline int ns_padded(int x) { return (int)ceil_div(x, dpg::NS_TILE) * dpg::NS_TILE; }
 inline int ns_planes(dp_dtype_t out_dt) { return out_dt == DP_BF16 ? 1 : 2; }
 
-// Checks the sizes and strides; *bytes gets the workspace the group needs.
+// The launches of a group: up to NS_MAX_MATS matrices each, from *next on; the small ones
+// (dpg::ns_small) and the others apart.
+dpg::NsArgs ns_batch(const dp_matrix_t* m, int n, int pl, bool small, int* next) {
+  dpg::NsArgs a{};
+  for (; *next < n && a.n < dpg::NS_MAX_MATS; ++*next) {
+    const dp_matrix_t& x = m[*next];
+    if (dpg::ns_small(x.rows, x.cols, pl) != small) continue;
+    dpg::NsMat& M = a.M[a.n++];
+    M.G = x.G; M.out = x.out; M.ldg = x.ldg; M.ldo = x.ldo;
+    M.rows = x.rows; M.cols = x.cols; M.scale = x.scale;
+    const int s = std::min(x.rows, x.cols), l = std::max(x.rows, x.cols);
+    M.mp = small ? (int)ceil_div(s, 32) * 32 : ns_padded(s);
+    M.np = small ? (int)ceil_div(l, 32) * 32 : ns_padded(l);
+  }
+  return a;
+}
+
+// Bytes of a launch's matrices, and of the parts of split sums behind them.
+size_t ns_batch_bytes(const dpg::NsArgs& a, int pl) {
+  size_t bytes = align_up(dpg::ns_part_bytes(a, pl));
+  for (int l = 0; l < a.n; ++l) bytes += align_up(dpg::ns_bytes(a.M[l].mp, a.M[l].np, pl));
+  return bytes;
+}
+
+// Checks the sizes and strides; *bytes gets the workspace the group needs (its
+// launches follow one another, so they share it).
 dp_status_t check_matrices(const dp_matrix_t* m, int n, dp_dtype_t in_dt, dp_dtype_t out_dt,
                            size_t* bytes) {
   if (!m || n <= 0) return fail(DP_EINVAL, "no matrices");
   if (!dtype_ok(in_dt)) return fail(DP_EINVAL, "unknown dtype %d", (int)in_dt);
   if (!dtype_ok(out_dt)) return fail(DP_EINVAL, "unknown dtype %d", (int)out_dt);
-  *bytes = 0;
   for (int l = 0; l < n; ++l) {
     const dp_matrix_t& x = m[l];
     if (x.rows <= 0 || x.cols <= 0) return fail(DP_EINVAL, "matrix %d: empty", l);
@@ -76,8 +100,13 @@ dp_status_t check_matrices(const dp_matrix_t* m, int n, dp_dtype_t in_dt, dp_dty
       return fail(DP_EUNSUPPORTED, "matrix %d: a side exceeds %d", l, dpg::NS_MAX_SIDE);
     if (x.ldg < x.cols || x.ldo < x.cols)
       return fail(DP_EINVAL, "matrix %d: row stride smaller than its columns", l);
-    *bytes += align_up(dpg::ns_bytes(ns_padded(std::min(x.rows, x.cols)),
-                                     ns_padded(std::max(x.rows, x.cols)), ns_planes(out_dt)));
+    if ((int64_t)ns_padded(x.rows) * ns_padded(x.cols) >= dpg::NS_MAX_SIZE)
+      return fail(DP_EUNSUPPORTED, "matrix %d: 2^30 elements or more", l);
+  }
+  *bytes = 0;
+  for (int next = 0; next < n;) {
+    const dpg::NsArgs a = ns_batch(m, n, ns_planes(out_dt), false, &next);
+    if (a.n) *bytes = std::max(*bytes, ns_batch_bytes(a, ns_planes(out_dt)));
   }
   return DP_OK;
 }
@@ -254,26 +283,29 @@ dp_status_t dp_orthogonalize_grouped(const dp_matrix_t* matrices, int n, dp_dtyp
     if (!matrices[l].G || !matrices[l].out) return fail(DP_EINVAL, "matrix %d: G or out is NULL", l);
     if (!std::isfinite(matrices[l].scale)) return fail(DP_EINVAL, "matrix %d: scale is not finite", l);
   }
-  if (!workspace || workspace_bytes < need)
+  if (need && (!workspace || workspace_bytes < need))
     return fail(DP_EINVAL, "workspace of %zu bytes needed", need);
-  if (!aligned16(workspace)) return fail(DP_EINVAL, "workspace must be 16-byte aligned");
-  char* ws = static_cast<char*>(workspace);
-  for (int l0 = 0; l0 < n; l0 += dpg::NS_MAX_MATS) {
-    dpg::NsArgs a{};
-    a.n = std::min(n - l0, dpg::NS_MAX_MATS);
+  if (need && !aligned16(workspace)) return fail(DP_EINVAL, "workspace must be 16-byte aligned");
+  const int pl = ns_planes(out_dt);
+  for (int next = 0; next < n;) {
+    dpg::NsArgs a = ns_batch(matrices, n, pl, true, &next);
+    if (a.n == 0) break;
     a.out_dt = kdt(out_dt); a.accumulate = accumulate ? 1 : 0; a.eps = eps;
+    st = hip_status(dpg::launch_orthogonalize_small(a, kdt(in_dt), pl, coef, steps, as_stream(stream)),
+                    "orthogonalize launch");
+    if (st != DP_OK) return st;
+  }
+  for (int next = 0; next < n;) {
+    dpg::NsArgs a = ns_batch(matrices, n, pl, false, &next);
+    if (a.n == 0) break;
+    a.out_dt = kdt(out_dt); a.accumulate = accumulate ? 1 : 0; a.eps = eps;
+    char* ws = static_cast<char*>(workspace);
     for (int l = 0; l < a.n; ++l) {
-      const dp_matrix_t& x = matrices[l0 + l];
-      dpg::NsMat& M = a.M[l];
-      M.G = x.G; M.out = x.out; M.ldg = x.ldg; M.ldo = x.ldo;
-      M.rows = x.rows; M.cols = x.cols; M.scale = x.scale;
-      M.mp = ns_padded(std::min(x.rows, x.cols));
-      M.np = ns_padded(std::max(x.rows, x.cols));
-      M.ws = ws;
-      ws += align_up(dpg::ns_bytes(M.mp, M.np, ns_planes(out_dt)));
+      a.M[l].ws = ws;
+      ws += align_up(dpg::ns_bytes(a.M[l].mp, a.M[l].np, pl));
     }
-    st = hip_status(dpg::launch_orthogonalize(a, kdt(in_dt), ns_planes(out_dt), coef, steps,
-                                              as_stream(stream)),
+    a.part = reinterpret_cast<float*>(ws);
+    st = hip_status(dpg::launch_orthogonalize(a, kdt(in_dt), pl, coef, steps, as_stream(stream)),
                     "orthogonalize launch");
     if (st != DP_OK) return st;
   }

@@ -520,11 +520,12 @@ hipError_t launch_preference(const PreferenceArgs& a, int B, hipStream_t s);
 
 // ---------------------------------------------------- orthogonalised updates
 constexpr int NS_TILE = 128;        // rows and columns of an output tile; sizes are padded to it
-constexpr int NS_MAX_MATS = 56;     // matrices per launch (kernel arguments stay < 4 KiB)
+constexpr int NS_MAX_MATS = 48;     // matrices per launch (kernel arguments stay < 4 KiB)
 constexpr int NS_MAX_SIDE = 65536;
+constexpr int64_t NS_MAX_SIZE = (int64_t)1 << 30;   // padded elements: a plane spans less than 2 GiB
 constexpr int NS_MAX_STEPS = 64;
-enum { NS_GRAM = 0, NS_POLY = 1, NS_UPDATE = 2 };                    // the three products of a step
-enum { NS_X = 0, NS_XT0 = 1, NS_XT1 = 2, NS_A = 3, NS_P = 4 };       // a matrix's buffers
+enum { NS_GRAM = 0, NS_POLY = 1, NS_UPDATE = 2, NS_LAST = 3 };       // the products of a step
+enum { NS_Y0 = 0, NS_Y1 = 1, NS_A = 2, NS_P = 3 };                   // a matrix's buffers
 
 struct NsMat {
   const void* G;        // [rows, ldg]
@@ -543,8 +544,16 @@ struct NsArgs {
   int32_t step, last;
   float coef[3];
   float eps;
+  uint32_t xcd_begin[9];  // items of XCD x: [xcd_begin[x], xcd_begin[x + 1])
+  int32_t ks;             // ranges of k of a symmetric product's tile
+  float* part;            // their sums, 64 KB each
+  int32_t steps;          // small matrices: all of them
 };
-static_assert(sizeof(NsArgs) <= 4096, "kernel arguments must stay within 4 KiB");
+constexpr int NS_COEFS = 3 * NS_MAX_STEPS;
+struct NsCoefs {
+  float c[NS_COEFS];
+};
+static_assert(sizeof(NsArgs) + 4 * 3 * NS_MAX_STEPS <= 4096, "kernel arguments must stay within 4 KiB");
 static_assert(NS_MAX_MATS <= 64, "a wave finds a work item's matrix with one lane per entry");
 
 constexpr int NS_PARTS = 128;       // most partial sums of squares of a matrix
@@ -555,16 +564,99 @@ DPG_HD inline int ns_parts(int rows, int cols) {
   const int64_t p = ((int64_t)rows * cols + 32767) / 32768;
   return p < 1 ? 1 : p > NS_PARTS ? NS_PARTS : (int)p;
 }
-// Offset of plane `plane` (of pl) of buffer `which`: X [mp, np], X^T [np, mp] twice, A and P [mp, mp].
+// Offset of plane `plane` (of pl) of buffer `which`: X^T [np, mp] twice, A and P [mp, mp].
 DPG_HD inline size_t ns_offset(int mp, int np, int which, int plane, int pl) {
-  const size_t x = (size_t)mp * np * 2, q = (size_t)mp * mp * 2;
-  const size_t at = which <= NS_A ? (size_t)which * pl * x : 3 * (size_t)pl * x + (size_t)pl * q;
-  return NS_HEAD + at + (size_t)plane * (which < NS_A ? x : q);
+  const size_t y = (size_t)mp * np * 2, q = (size_t)mp * mp * 2;
+  const size_t at = which <= NS_A ? (size_t)which * pl * y : 2 * (size_t)pl * y + (size_t)pl * q;
+  return NS_HEAD + at + (size_t)plane * (which < NS_A ? y : q);
 }
 DPG_HD inline size_t ns_bytes(int mp, int np, int pl) {
   return ns_offset(mp, np, NS_P, 0, pl) + (size_t)pl * mp * mp * 2;
 }
 #undef DPG_HD
+// Ranges of k that a symmetric product's tiles are cut into. One workgroup keeps a CU's
+// matrix cores as busy as two do (a second one only fills the first's gaps), so a launch
+// runs 256 items at a time, each for about its k and 600 more, US_K us per k; joining the
+// ranges is another launch. Cut where a launch fills at most half a round and that pays. (1601
+// x 6397, two planes, us: X X^T 103 whole and 67 + 9 in 5 ranges, A^2 35 and 20 + 8 in 2; 2048 x
+// 8192, one plane, 136 tiles: 75 whole, 58 + 13 in 3.)
+constexpr double NS_JOIN_US = 8.0;
+inline int ns_split(const NsArgs& a, int kind, int pl) {
+  const double us_k = pl == 1 ? 0.008 : 0.0136;
+  int64_t tiles = 0, k_most = 0, k_least = 1 << 30;
+  for (int l = 0; l < a.n; ++l) {
+    const int64_t t = (a.M[l].mp + NS_TILE - 1) / NS_TILE, k = kind == NS_GRAM ? a.M[l].np : a.M[l].mp;
+    tiles += t * (t + 1) / 2;
+    k_most = k > k_most ? k : k_most;
+    k_least = k < k_least ? k : k_least;
+  }
+  if (tiles > 128) return 1;
+  int best = 1;
+  double best_us = (double)(k_most + 600) * us_k;
+  for (int ks = 2; ks <= 16 && ks * 128 <= k_least; ++ks) {
+    const double us = (double)((tiles * ks + 255) / 256) * ((double)k_most / ks + 600) * us_k + NS_JOIN_US;
+    if (us < 0.95 * best_us) { best_us = us; best = ks; }
+  }
+  return best;
+}
+inline size_t ns_part_bytes(const NsArgs& a, int pl) {
+  size_t most = 0;
+  for (int kind = NS_GRAM; kind <= NS_POLY; ++kind) {
+    const int ks = ns_split(a, kind, pl);
+    if (ks == 1) continue;
+    size_t tiles = 0;
+    for (int l = 0; l < a.n; ++l) {
+      const size_t t = (size_t)(a.M[l].mp + NS_TILE - 1) / NS_TILE;
+      tiles += t * (t + 1) / 2;
+    }
+    const size_t n = tiles * ks * NS_TILE * NS_TILE * 4;
+    most = n > most ? n : most;
+  }
+  return most;
+}
+
+// Reorders the matrices so that 8 bins, one per XCD, of consecutive ones have nearly equal
+// work, the longest sums first in each (longest first, each to the emptiest bin).
+struct NsBins {
+  int begin[9];
+};
+inline NsBins ns_order(NsArgs& a) {
+  int by[NS_MAX_MATS], bin[NS_MAX_MATS];
+  double load[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+  auto work = [&](int l) { return (double)a.M[l].mp * a.M[l].mp * a.M[l].np; };
+  for (int l = 0; l < a.n; ++l) {   // insertion sort: stable, and short
+    int k = l;
+    while (k > 0 && work(by[k - 1]) < work(l)) { by[k] = by[k - 1]; --k; }
+    by[k] = l;
+  }
+  for (int k = 0; k < a.n; ++k) {
+    int x = 0;
+    for (int q = 1; q < 8; ++q) x = load[q] < load[x] ? q : x;
+    bin[k] = x;
+    load[x] += work(by[k]);
+  }
+  NsBins b;
+  NsMat sorted[NS_MAX_MATS];
+  int n = 0;
+  for (int x = 0; x < 8; ++x) {
+    b.begin[x] = n;
+    for (int k = 0; k < a.n; ++k)
+      if (bin[k] == x) sorted[n++] = a.M[by[k]];
+  }
+  b.begin[8] = n;
+  for (int l = 0; l < n; ++l) a.M[l] = sorted[l];
+  return b;
+}
+// Matrices small enough for one workgroup to keep X, A and P in its LDS take all their
+// steps there (mp, np: sides padded to 32; no workspace).
+constexpr int NS_SMALL_WAVES = 8, NS_SMALL_BLOCKS = 4;   // waves; most 32 x 32 blocks of X per wave
+constexpr int NS_SMALL_LDS = 160 * 1024 - NS_SMALL_WAVES * 32 * 36 * 4 - 256;
+inline bool ns_small(int rows, int cols, int pl) {
+  const int64_t r = (rows + 31) / 32 * 32, c = (cols + 31) / 32 * 32, m = r < c ? r : c, n = r < c ? c : r;
+  return 2 * pl * (n * m + 2 * m * m) <= NS_SMALL_LDS && n * m <= 1024 * NS_SMALL_WAVES * NS_SMALL_BLOCKS;
+}
+hipError_t launch_orthogonalize_small(const NsArgs& a, int dt, int planes, const float* coef, int steps,
+                                      hipStream_t s);
 hipError_t launch_orthogonalize(const NsArgs& a, int dt, int planes, const float* coef, int steps,
                                 hipStream_t s);
 

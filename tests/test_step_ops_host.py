@@ -170,7 +170,7 @@ def test_layernorm_formula_against_autograd():
     np.testing.assert_allclose(back["dbias"].sum(0), bias.grad.numpy(), rtol=1e-11)
 
 
-def _matrix(G=P[0], ldg=64, out=P[1], ldo=64, rows=32, cols=64, scale=1.0):
+def _matrix(G=P[0], ldg=640, out=P[1], ldo=640, rows=320, cols=640, scale=1.0):
     return D.dp_matrix_t(G, ldg, out, ldo, rows, cols, scale)
 
 
@@ -187,7 +187,7 @@ def _orth(L, m=None, n=1, dt=0, odt=0, coef=(1.0, 2.0, 3.0), steps=1, eps=0.0, w
     (dict(steps=65, coef=(0.0,) * 195), EINVAL), (dict(eps=-1.0), EINVAL),
     (dict(eps=float("inf")), EINVAL), (dict(ws=None), EINVAL), (dict(nbytes=64), EINVAL),
     (dict(ws=P[2] + 2), EINVAL), (dict(m=_matrix(G=None)), EINVAL), (dict(m=_matrix(out=None)), EINVAL),
-    (dict(m=_matrix(ldg=63)), EINVAL), (dict(m=_matrix(ldo=63)), EINVAL),
+    (dict(m=_matrix(ldg=639)), EINVAL), (dict(m=_matrix(ldo=639)), EINVAL),
     (dict(m=_matrix(rows=0)), EINVAL), (dict(m=_matrix(cols=-1)), EINVAL),
     (dict(m=_matrix(scale=float("nan"))), EINVAL), (dict(m=_matrix(rows=65537)), EUNSUP),
     (dict(m=_matrix(cols=65537, ldg=65537, ldo=65537)), EUNSUP)])
@@ -196,10 +196,12 @@ def test_orthogonalize_refuses(L, kw, status):
 
 
 def test_orthogonalize_workspace(L):
-    one, tall = (D.dp_matrix_t * 1)(_matrix()), (D.dp_matrix_t * 1)(_matrix(rows=64, cols=32, ldg=32, ldo=32))
+    one, tall = (D.dp_matrix_t * 1)(_matrix()), (D.dp_matrix_t * 1)(_matrix(rows=640, cols=320, ldg=320, ldo=320))
     assert L.dp_orthogonalize_workspace(one, 1, D.DP_BF16) == L.dp_orthogonalize_workspace(tall, 1, D.DP_BF16)
     assert L.dp_orthogonalize_workspace(one, 1, D.DP_F32) > L.dp_orthogonalize_workspace(one, 1, D.DP_BF16) > 0
     assert L.dp_orthogonalize_workspace(None, 1, D.DP_F32) == 0
+    small = (D.dp_matrix_t * 1)(_matrix(rows=64, cols=256))      # worked in LDS
+    assert L.dp_orthogonalize_workspace(small, 1, D.DP_F32) == 0
     assert L.dp_orthogonalize_workspace(one, 0, D.DP_F32) == 0
 
 
