@@ -671,18 +671,23 @@ __global__ __launch_bounds__(NS_SMALL_WAVES * WAVE) void ns_small_kernel(NsArgs 
   // A block's sum over ks steps of 16 k; fp(p, k), fq(p, k): the operands' planes.
   auto product = [&](int ks, auto fp, auto fq) __attribute__((always_inline)) {
     f32x16 big = {}, little = {};
-    for (int k = 0; k < ks; ++k) {
-      u32x4 x[PL], y[PL];
+    for (int k = 0; k < ks; k += 2) {   // ks is even: the reads of two steps are in flight together
+      u32x4 x[2][PL], y[2][PL];
 #pragma unroll
-      for (int p = 0; p < PL; ++p) {
-        x[p] = fp(p, k);
-        y[p] = fq(p, k);
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int p = 0; p < PL; ++p) {
+          x[u][p] = fp(p, k + u);
+          y[u][p] = fq(p, k + u);
+        }
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        if constexpr (PL == 2) {
+          little = mfma32_f16(x[u][1], y[u][0], little);
+          little = mfma32_f16(x[u][0], y[u][1], little);
+        }
+        big = mfma32_f16(x[u][0], y[u][0], big);
       }
-      if constexpr (PL == 2) {
-        little = mfma32_f16(x[1], y[0], little);
-        little = mfma32_f16(x[0], y[1], little);
-      }
-      big = mfma32_f16(x[0], y[0], big);
     }
     if constexpr (PL == 2) big += little;
     return big;
@@ -725,9 +730,10 @@ __global__ __launch_bounds__(NS_SMALL_WAVES * WAVE) void ns_small_kernel(NsArgs 
 #pragma unroll
     for (int kind = NS_GRAM; kind <= NS_POLY; ++kind) {
       __syncthreads();
-      for (int t = w; t < mb * (mb + 1) / 2; t += W) {
-        int ti, tj;
-        ns_triangle((uint32_t)t, ti, tj);
+      // All blocks: the mirrored ones cost a wave without work of its own nothing, where
+      // storing a block twice would be another turn through the slice.
+      for (int t = w; t < mb * mb; t += W) {
+        const int ti = t / mb, tj = t % mb;
         const f32x16 c =
             kind == NS_GRAM
                 ? product(np / 16, [&](int p, int k) { return cols(Y + p * planeY, ti, k); },
@@ -737,11 +743,6 @@ __global__ __launch_bounds__(NS_SMALL_WAVES * WAVE) void ns_small_kernel(NsArgs 
         ns_fill<false>(slice, c, lane);
         if (kind == NS_GRAM) keep(A, planeA, 32 * tj, 32 * ti, times(NS_SA / (NS_SX * NS_SX)));
         else keep(P, planeA, 32 * tj, 32 * ti, poly);
-        if (ti != tj) {
-          ns_fill<true>(slice, c, lane);
-          if (kind == NS_GRAM) keep(A, planeA, 32 * ti, 32 * tj, times(NS_SA / (NS_SX * NS_SX)));
-          else keep(P, planeA, 32 * ti, 32 * tj, poly);
-        }
       }
     }
     __syncthreads();
