@@ -239,7 +239,7 @@ dp_status_t dp_preference_loss(const void* Z, int64_t ldz, const int32_t* target
   a.stat = reinterpret_cast<dpg::RowStat*>(ws + l.stat);
   a.w = reinterpret_cast<float*>(ws + l.slope);
   a.V = V; a.T = T; a.split = split;
-  const int64_t pairs = dpg::preference_pairs(B, T, V, esize(dt));
+  const int64_t pairs = dpg::preference_pairs(B, T, V);
   for (int64_t b = 0; b < B; b += pairs) {
     const int64_t n = std::min<int64_t>(pairs, B - b);
     a.row0 = b * T;

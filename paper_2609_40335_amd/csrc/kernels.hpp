@@ -460,20 +460,22 @@ hipError_t launch_ln_backward(const LnBackwardArgs& a, int dt, hipStream_t s);
 // How the backward pass cuts an example's T rows: about LN_GROUPS workgroups in
 // all, but no fewer rows each than keep the partial sums' way to memory and back
 // (16 d bytes a range) below a quarter of the operands' (3 T d elements).
-constexpr int LN_GROUPS = 1024;
+constexpr int LN_GROUPS = 512, LN_FEW = 32;
 struct LnPlan {
   int32_t ranges, span, chunks;
 };
 inline LnPlan ln_plan(int B, int T, int d, bool grads) {
   const int teams = d <= 2048 ? 8 : 1;
   const int least = grads ? (teams > 1 ? 2 * teams : 8) : teams;
-  int64_t ranges = (LN_GROUPS + B - 1) / B, most = (T + least - 1) / least;
+  const int groups = d <= 2048 ? LN_GROUPS : d <= 4096 ? 4 * LN_GROUPS : LN_GROUPS;
+  int64_t ranges = (groups + B - 1) / B, most = (T + least - 1) / least;
   if (ranges > most) ranges = most;
   LnPlan p;
   p.span = (int32_t)((T + ranges - 1) / ranges);
   p.ranges = (T + p.span - 1) / p.span;
-  // One workgroup per example adds up to this many partial sums itself.
-  p.chunks = (int64_t)p.ranges * d <= 16384 ? 1 : (d + 63) / 64;
+  // One workgroup per example adds few ranges (a chain of loads each); more are added by
+  // chunks of 64 features, and an example's norm by a third launch.
+  p.chunks = p.ranges <= LN_FEW ? 1 : (d + 63) / 64;
   return p;
 }
 
@@ -510,9 +512,10 @@ struct PreferenceArgs {
   int32_t T, V, split;
   float beta, smoothing;
 };
-// Pairs of one pass: workgroups are counted in 32 bits.
-inline int64_t preference_pairs(int B, int T, int V, int es) {
-  (void)es;
+// Pairs of one pass: workgroups are counted in 32 bits. (Fewer at a time, so that the second
+// read meets the memory-side cache, was no gain: 16 pairs of 1024 rows of 50257 in bf16 take 652 us in
+// one pass, 688 two at a time, 832 one by one, for the launches' ends.)
+inline int64_t preference_pairs(int B, int T, int V) {
   const int64_t most = ((int64_t)1 << 30) / ((int64_t)T * ((V + 8191) / 8192));
   return most < 1 ? 1 : most < B ? most : B;
 }

@@ -12,7 +12,7 @@
 //
 // Both passes are bound by HBM: 2 (forward) or 3 (backward) elements a feature.
 // A row is read once into the registers of a team, one wave up to 2048
-// features (its sums need no barrier), 4 waves up to 8192, 16 up to 32768, and
+// features (its sums need no barrier), 4 waves up to 4096, 16 up to 32768, and
 // both sums of a row meet in one exchange. A lane holds the same features of
 // every row it meets, so the token sums of dgain and dbias stay in its
 // registers; a workgroup covers a range of an example's rows, and ranges are
@@ -31,10 +31,33 @@ struct LnTeam {
   static constexpr int TEAMS = W == 1 ? LN_WAVES : 1;
 };
 
-// A parameter of either type; a null one is `one`.
-__device__ __forceinline__ float ln_param(const void* p, int dt, int64_t col, float none) {
-  if (!p) return none;
-  return dt == DT_BF16 ? bf16_to_f32(((const uint16_t*)p)[col]) : ((const float*)p)[col];
+// Eight of a parameter's d elements of either type from col on; a null one is `none`.
+__device__ __forceinline__ void ln_params(const void* p, int dt, int col, int d, float none, float (&v)[8]) {
+  if (!p) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = none;
+  } else if (dt == DT_BF16) {
+    Oct<DT_BF16> o;
+    o.load((const char*)p + (int64_t)col * 2, d - col);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = o.at(e);
+  } else {
+    Oct<DT_F32> o;
+    o.load((const char*)p + (int64_t)col * 4, d - col);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = o.at(e);
+  }
+}
+
+// A lane's octets of a row.
+template <int DT, int W, int NV>
+__device__ __forceinline__ void ln_load(const void* base, int64_t ld, int64_t row, int lane, int d, Oct<DT> (&v)[NV]) {
+  const char* p = (const char*)base + row * ld * Oct<DT>::ES;
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    const int col = (lane + j * W * WAVE) * 8;
+    v[j].load(p + (int64_t)col * Oct<DT>::ES, d - col);
+  }
 }
 
 template <int DT, int W, int NV>
@@ -44,26 +67,24 @@ __global__ __launch_bounds__(LnTeam<W>::THREADS) void ln_forward_kernel(LnForwar
   const int lane = (int)threadIdx.x % LANES, team = (int)threadIdx.x / LANES;
   const int d = a.d;
   const float inv_d = 1.f / (float)d;
+  const int64_t step = (int64_t)gridDim.x * LnTeam<W>::TEAMS;
+  int64_t row = (int64_t)blockIdx.x * LnTeam<W>::TEAMS + team;
+  if (row >= a.rows) return;   // a whole team
+  Oct<DT> v[NV], next[NV];
+  ln_load<DT, W, NV>(a.x, a.ldx, row, lane, d, v);
   float gain[NV][8], bias[NV][8];
 #pragma unroll
-  for (int j = 0; j < NV; ++j)
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const int col = (lane + j * LANES) * 8 + e;
-      gain[j][e] = col < d ? ln_param(a.gain, a.param_dt, col, 1.f) : 0.f;
-      bias[j][e] = col < d ? ln_param(a.bias, a.param_dt, col, 0.f) : 0.f;
-    }
-  for (int64_t row = (int64_t)blockIdx.x * LnTeam<W>::TEAMS + team; row < a.rows;
-       row += (int64_t)gridDim.x * LnTeam<W>::TEAMS) {
-    const char* x = (const char*)a.x + row * a.ldx * Oct<DT>::ES;
+  for (int j = 0; j < NV; ++j) {
+    ln_params(a.gain, a.param_dt, (lane + j * LANES) * 8, d, 1.f, gain[j]);
+    ln_params(a.bias, a.param_dt, (lane + j * LANES) * 8, d, 0.f, bias[j]);
+  }
+  for (; row < a.rows; row += step) {
+    // The next row is on its way while this one is worked on.
+    const bool more = row + step < a.rows;
+    constexpr bool AHEAD = NV <= 2 && NV * W <= 16;
+    if (AHEAD && more) ln_load<DT, W, NV>(a.x, a.ldx, row + step, lane, d, next);
     char* y = (char*)a.y + row * a.ldy * Oct<DT>::ES;
-    Oct<DT> v[NV];
     float sum = 0.f, none = 0.f;
-#pragma unroll
-    for (int j = 0; j < NV; ++j) {
-      const int col = (lane + j * LANES) * 8;
-      v[j].load(x + (int64_t)col * Oct<DT>::ES, d - col);
-    }
 #pragma unroll
     for (int j = 0; j < NV; ++j)
 #pragma unroll
@@ -100,6 +121,14 @@ __global__ __launch_bounds__(LnTeam<W>::THREADS) void ln_forward_kernel(LnForwar
       if (a.mean) a.mean[row] = mean;
       if (a.rstd) a.rstd[row] = rstd;
     }
+    if (more) {
+      if constexpr (AHEAD) {
+#pragma unroll
+        for (int j = 0; j < NV; ++j) v[j] = next[j];
+      } else {
+        ln_load<DT, W, NV>(a.x, a.ldx, row + step, lane, d, v);
+      }
+    }
   }
 }
 
@@ -116,28 +145,32 @@ __global__ __launch_bounds__(LnTeam<W>::THREADS) void ln_backward_kernel(LnBackw
   const int d = a.d;
   const float inv_d = 1.f / (float)d;
   const int t0 = s * a.span, t1 = min(t0 + a.span, a.T);
+  const int64_t row0 = (int64_t)b * a.T;
+  Oct<DT> x[NV], g[NV];
+  float mean = 0.f, rstd = 0.f;
+  auto fetch = [&](int t, Oct<DT> (&px)[NV], Oct<DT> (&pg)[NV], float& m, float& r) __attribute__((always_inline)) {
+    ln_load<DT, W, NV>(a.x, a.ldx, row0 + t, lane, d, px);
+    ln_load<DT, W, NV>(a.gy, a.ldgy, row0 + t, lane, d, pg);
+    m = a.mean[row0 + t];
+    r = a.rstd[row0 + t];
+  };
+  if (t0 + team < t1) fetch(t0 + team, x, g, mean, rstd);
   float gain[NV][8];
   float dg[NV][8], db[NV][8];
 #pragma unroll
-  for (int j = 0; j < NV; ++j)
+  for (int j = 0; j < NV; ++j) {
+    if constexpr (DX) ln_params(a.gain, a.param_dt, (lane + j * LANES) * 8, d, 1.f, gain[j]);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const int col = (lane + j * LANES) * 8 + e;
-      gain[j][e] = DX && col < d ? ln_param(a.gain, a.param_dt, col, 1.f) : 0.f;
-      dg[j][e] = db[j][e] = 0.f;
-    }
+    for (int e = 0; e < 8; ++e) dg[j][e] = db[j][e] = 0.f;
+  }
   for (int t = t0 + team; t < t1; t += TEAMS) {
-    const int64_t row = (int64_t)b * a.T + t;
-    const char* px = (const char*)a.x + row * a.ldx * Oct<DT>::ES;
-    const char* pg = (const char*)a.gy + row * a.ldgy * Oct<DT>::ES;
-    Oct<DT> x[NV], g[NV];
-#pragma unroll
-    for (int j = 0; j < NV; ++j) {
-      const int col = (lane + j * LANES) * 8;
-      x[j].load(px + (int64_t)col * Oct<DT>::ES, d - col);
-      g[j].load(pg + (int64_t)col * Oct<DT>::ES, d - col);
-    }
-    const float mean = a.mean[row], rstd = a.rstd[row];
+    const int64_t row = row0 + t;
+    // The next row is on its way while this one is worked on, where registers allow.
+    constexpr bool AHEAD = NV <= 2 && NV * W <= 16;
+    Oct<DT> nx[NV], ng[NV];
+    float nm = 0.f, nr = 0.f;
+    const bool more = t + TEAMS < t1;
+    if (AHEAD && more) fetch(t + TEAMS, nx, ng, nm, nr);
     float s1 = 0.f, s2 = 0.f;
     // Features past d have gy = 0 here, so their xhat drops out of every sum.
 #pragma unroll
@@ -176,6 +209,19 @@ __global__ __launch_bounds__(LnTeam<W>::THREADS) void ln_backward_kernel(LnBackw
         }
         x[j].set(o);
         x[j].store(pd + (int64_t)col * Oct<DT>::ES, d - col);
+      }
+    }
+    if (more) {
+      if constexpr (AHEAD) {
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+          x[j] = nx[j];
+          g[j] = ng[j];
+        }
+        mean = nm;
+        rstd = nr;
+      } else {
+        fetch(t + TEAMS, x, g, mean, rstd);
       }
     }
   }
@@ -229,53 +275,76 @@ __global__ __launch_bounds__(LnTeam<W>::THREADS) void ln_backward_kernel(LnBackw
 }
 static_assert(LN_WAVES == 8, "a team per element of an octet");
 
-// The ranges' partial sums of example blockIdx.y, 64 features at a time by
-// 4 groups of threads that each add every fourth range (then the groups, in
-// order). One workgroup per example writes the norm itself; several leave
-// a partial each.
-__global__ __launch_bounds__(256) void ln_finish_kernel(LnBackwardArgs a) {
-  __shared__ float meet[4][2][64];
-  __shared__ float sq_red[4];
-  const int b = (int)blockIdx.y, c = (int)threadIdx.x % 64, grp = (int)threadIdx.x / 64;
-  const int d = a.d;
+// The ranges' partial sums of example blockIdx.y. FEW (at most LN_FEW ranges): a thread adds
+// a feature's, in order, one workgroup per example, which writes the norm too. Otherwise
+// LN_FIN_COLS features a workgroup, by 16 groups of threads that each add every
+// sixteenth range (then the groups, in order); each leaves a partial of the norm.
+constexpr int LN_FIN_COLS = 64, LN_FIN_GROUPS = 16, LN_FIN_THREADS = LN_FIN_COLS * LN_FIN_GROUPS;
+template <bool FEW>
+__global__ __launch_bounds__(LN_FIN_THREADS) void ln_finish_kernel(LnBackwardArgs a) {
+  const int b = (int)blockIdx.y, d = a.d;
   const float* ws = a.ws + (int64_t)b * a.ranges * 2 * d;
   float sq = 0.f;
-  for (int c0 = (int)blockIdx.x * 64; c0 < d; c0 += (int)gridDim.x * 64) {
-    const int col = c0 + c;
+  auto put = [&](int col, float vg, float vb) {
+    if (a.dgain) { a.dgain[(int64_t)b * d + col] = vg; sq = fmaf(vg, vg, sq); }
+    if (a.dbias) { a.dbias[(int64_t)b * d + col] = vb; sq = fmaf(vb, vb, sq); }
+  };
+  if constexpr (FEW) {
+    __shared__ float red[LN_FIN_THREADS / WAVE];
+    for (int col = (int)threadIdx.x; col < d; col += LN_FIN_THREADS) {
+      float vg = 0.f, vb = 0.f;
+#pragma unroll 8
+      for (int s = 0; s < a.ranges; ++s) {
+        vg += ws[(int64_t)s * 2 * d + col];
+        vb += ws[(int64_t)s * 2 * d + d + col];
+      }
+      put(col, vg, vb);
+    }
+    if (!a.norm2) return;
+    sq = wave_sum(sq);
+    if (threadIdx.x % WAVE == 0) red[threadIdx.x / WAVE] = sq;
+    __syncthreads();
+    if (threadIdx.x != 0) return;
+    sq = 0.f;
+    for (int w = 0; w < LN_FIN_THREADS / WAVE; ++w) sq += red[w];
+    a.norm2[b] = (a.accumulate ? a.norm2[b] : 0.f) + sq;
+  } else {
+    __shared__ float meet[LN_FIN_GROUPS][2][LN_FIN_COLS];
+    const int c = (int)threadIdx.x % LN_FIN_COLS, grp = (int)threadIdx.x / LN_FIN_COLS;
+    const int col = (int)blockIdx.x * LN_FIN_COLS + c;
     float vg = 0.f, vb = 0.f;
     if (col < d) {
-#pragma unroll 4
-      for (int s = grp; s < a.ranges; s += 4) {
+#pragma unroll 8
+      for (int s = grp; s < a.ranges; s += LN_FIN_GROUPS) {
         vg += ws[(int64_t)s * 2 * d + col];
         vb += ws[(int64_t)s * 2 * d + d + col];
       }
     }
-    __syncthreads();
     meet[grp][0][c] = vg;
     meet[grp][1][c] = vb;
     __syncthreads();
-    if (grp == 0 && col < d) {
-      vg = meet[0][0][c] + meet[1][0][c] + meet[2][0][c] + meet[3][0][c];
-      vb = meet[0][1][c] + meet[1][1][c] + meet[2][1][c] + meet[3][1][c];
-      if (a.dgain) { a.dgain[(int64_t)b * d + col] = vg; sq = fmaf(vg, vg, sq); }
-      if (a.dbias) { a.dbias[(int64_t)b * d + col] = vb; sq = fmaf(vb, vb, sq); }
+    if (grp != 0) return;
+    if (col < d) {
+      vg = vb = 0.f;
+#pragma unroll
+      for (int q = 0; q < LN_FIN_GROUPS; ++q) {
+        vg += meet[q][0][c];
+        vb += meet[q][1][c];
+      }
+      put(col, vg, vb);
     }
-  }
-  if (!a.norm2) return;
-  sq = wave_sum(sq);   // only the first wave holds any
-  (void)sq_red;
-  if (threadIdx.x == 0) {
-    if (gridDim.x == 1)
-      a.norm2[b] = (a.accumulate ? a.norm2[b] : 0.f) + sq;
-    else
-      a.sq[(int64_t)b * gridDim.x + blockIdx.x] = sq;
+    if (!a.norm2) return;
+    sq = wave_sum(sq);
+    if (threadIdx.x == 0) a.sq[(int64_t)b * gridDim.x + blockIdx.x] = sq;
   }
 }
 
 template <int DT, int W, int NV>
 static hipError_t ln_forward(const LnForwardArgs& a, hipStream_t s) {
   const int64_t need = (a.rows + LnTeam<W>::TEAMS - 1) / LnTeam<W>::TEAMS;
-  const unsigned grid = (unsigned)(need < 2048 ? need : 2048);
+  // As many workgroups as the registers let the GPU hold: rows beyond are prefetched.
+  constexpr int64_t MOST = 256 * (W == 1 ? (NV == 1 ? 4 : NV == 2 ? 3 : 2) : W == 4 ? 4 : 2);
+  const unsigned grid = (unsigned)(need < MOST ? need : MOST);
   hipLaunchKernelGGL((ln_forward_kernel<DT, W, NV>), dim3(grid), dim3(LnTeam<W>::THREADS), 0, s, a);
   return hipGetLastError();
 }
@@ -292,9 +361,14 @@ static hipError_t ln_backward(const LnBackwardArgs& a, hipStream_t s) {
     hipLaunchKernelGGL((ln_backward_kernel<DT, W, NV, false, true>), grid, block, 0, s, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.ranges == 1 || !wg) return e;
-  hipLaunchKernelGGL(ln_finish_kernel, dim3((unsigned)a.chunks, (unsigned)a.B), dim3(256), 0, s, a);
+  const dim3 fin(LN_FIN_THREADS);
+  if (a.chunks == 1) {
+    hipLaunchKernelGGL((ln_finish_kernel<true>), dim3(1, (unsigned)a.B), fin, 0, s, a);
+    return hipGetLastError();
+  }
+  hipLaunchKernelGGL((ln_finish_kernel<false>), dim3((unsigned)a.chunks, (unsigned)a.B), fin, 0, s, a);
   e = hipGetLastError();
-  if (e != hipSuccess || !a.norm2 || a.chunks == 1) return e;
+  if (e != hipSuccess || !a.norm2) return e;
   return launch_finish_rows(a.sq, a.B, a.chunks, a.norm2, a.accumulate, 1.f, s);
 }
 
@@ -306,7 +380,7 @@ static hipError_t ln_backward(const LnBackwardArgs& a, hipStream_t s) {
     if (octs <= 128) return FN<DT, 1, 2>(a, s);    \
     if (octs <= 256) return FN<DT, 1, 4>(a, s);    \
     if (octs <= 512) return FN<DT, 4, 2>(a, s);    \
-    if (octs <= 1024) return FN<DT, 4, 4>(a, s);   \
+    if (octs <= 1024) return FN<DT, 16, 1>(a, s);  \
     if (octs <= 2048) return FN<DT, 16, 2>(a, s);  \
     return FN<DT, 16, 4>(a, s);                    \
   } while (0)

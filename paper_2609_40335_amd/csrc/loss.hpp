@@ -34,8 +34,14 @@ constexpr float LOWEST = -FLT_MAX;   // running maximum of no logits (finite: -i
 template <int DT>
 constexpr uint32_t NEG_INF = DT == DT_BF16 ? 0xFF80FF80u : 0xFF800000u;
 
+// EXACT: log2 e in two parts. As one fp32 number it is 1.3e-8 of itself off, the same way in
+// every row, which a sum of hundreds of log-probabilities shows.
+template <bool EXACT>
 __device__ __forceinline__ float exp_from(float z, float top) {
-  return __builtin_amdgcn_exp2f((z - top) * LOG2E);
+  constexpr float LO = (float)(1.4426950408889634 - (double)LOG2E);
+  static_assert(LO > 0.f, "-inf LO is -inf");
+  const float d = z - top;
+  return __builtin_amdgcn_exp2f(EXACT ? fmaf(d, LO, d * LOG2E) : d * LOG2E);
 }
 
 __device__ __forceinline__ float wave_max(float v) {
@@ -67,8 +73,10 @@ struct LossTeam {
 };
 
 // Running maximum and sum of exponentials of the lane's logits: octets `lane`,
-// `lane` + LANES, ... of the row, U of them in flight.
-template <int DT, int W, int U>
+// `lane` + LANES, ... of the row, U of them in flight. EXACT rows are read a second time soon, others take
+// streaming loads in bf16 (24 x 128 rows of 50257: 57 us without the hint, 55 with; in fp32, where a lane's octet is two
+// loads of the same line, 83 and 101).
+template <int DT, int W, int U, bool EXACT>
 __device__ __forceinline__ void row_sum(const char* z, int V, int lane, float& top, float& sum) {
   constexpr int LANES = W * WAVE;
   top = LOWEST;
@@ -78,27 +86,27 @@ __device__ __forceinline__ void row_sum(const char* z, int V, int lane, float& t
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int col = (o + u * LANES) * 8;
-      v[u].load(z + (int64_t)col * Oct<DT>::ES, V - col, NEG_INF<DT>);
+      v[u].template load<!EXACT && DT == DT_BF16>(z + (int64_t)col * Oct<DT>::ES, V - col, NEG_INF<DT>);
     }
     float m = top;
 #pragma unroll
     for (int u = 0; u < U; ++u)
 #pragma unroll
       for (int e = 0; e < 8; ++e) m = fmaxf(m, v[u].at(e));
-    sum *= exp_from(top, m);
+    sum *= exp_from<EXACT>(top, m);
 #pragma unroll
     for (int u = 0; u < U; ++u)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) sum += exp_from(v[u].at(e), m);
+      for (int e = 0; e < 8; ++e) sum += exp_from<EXACT>(v[u].at(e), m);
     top = m;
   }
 }
 
 // The team's: every thread gets the row's maximum and sum.
-template <int W>
+template <int W, bool EXACT>
 __device__ __forceinline__ void team_row(float& top, float& sum, float* red) {
   const float m = team_max<W>(top, red);
-  float s = sum * exp_from(top, m), none = 0.f;
+  float s = sum * exp_from<EXACT>(top, m), none = 0.f;
   team_sum2<W>(s, none, red);
   top = m;
   sum = s;
@@ -114,7 +122,7 @@ __device__ __forceinline__ float logit_at(const char* z, int col) {
   else return ((const float*)z)[col];
 }
 
-template <int DT, int W>
+template <int DT, int W, int U, bool EXACT>
 __global__ __launch_bounds__(LossTeam<W>::THREADS) void token_logprobs_kernel(LossArgs a) {
   __shared__ float red[2 * W];
   const int lane = (int)threadIdx.x % (W * WAVE), team = (int)threadIdx.x / (W * WAVE);
@@ -134,8 +142,8 @@ __global__ __launch_bounds__(LossTeam<W>::THREADS) void token_logprobs_kernel(Lo
   const char* z = (const char*)a.Z + row * a.ldz * Oct<DT>::ES;
   const float zt = logit_at<DT>(z, y);
   float top, sum;
-  row_sum<DT, W, 4>(z, a.V, lane, top, sum);
-  team_row<W>(top, sum, red);
+  row_sum<DT, W, U, EXACT>(z, a.V, lane, top, sum);
+  team_row<W, EXACT>(top, sum, red);
   if (lane == 0) {
     const double logp = row_logp(zt, top, sum);
     if (a.logp) a.logp[row] = (float)logp;
@@ -145,28 +153,41 @@ __global__ __launch_bounds__(LossTeam<W>::THREADS) void token_logprobs_kernel(Lo
   }
 }
 
-// Eight gradients w (p - onehot) of an octet that starts at column col.
+// Eight gradients w p of an octet, f = w / sum. The target's is put right afterwards, by
+// the thread that stored it.
 template <int DT>
-__device__ __forceinline__ void grad_octet(Oct<DT>& v, float top, float f, float w, int rel) {
+__device__ __forceinline__ void grad_octet(Oct<DT>& v, float top, float f) {
   float o[8];
 #pragma unroll
-  for (int e = 0; e < 8; ++e) o[e] = fmaf(exp_from(v.at(e), top), f, e == rel ? -w : 0.f);
+  for (int e = 0; e < 8; ++e) o[e] = exp_from<false>(v.at(e), top) * f;
   v.set(o);
+}
+template <int DT>
+__device__ __forceinline__ void grad_target(char* g, int y, float zt, float top, float f, float w) {
+  const float v = fmaf(exp_from<false>(zt, top), f, -w);
+  if constexpr (DT == DT_BF16)
+    ((uint16_t*)g)[y] = (uint16_t)__builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{v, v}, bf16x2));
+  else
+    ((float*)g)[y] = v;
 }
 
 // Rows that give no gradient: octets from `lane` on, LANES apart.
-template <int DT>
+template <int DT, bool NT>
 __device__ __forceinline__ void zero_row(char* g, int V, int lane, int lanes) {
   Oct<DT> v;
   const float none[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
   v.set(none);
-  for (int col = lane * 8; col < V; col += lanes * 8) v.store(g + (int64_t)col * Oct<DT>::ES, V - col);
+  for (int col = lane * 8; col < V; col += lanes * 8) v.template store<NT>(g + (int64_t)col * Oct<DT>::ES, V - col);
 }
 
 // NV > 0: the row stays in registers, NV octets a lane. NV = 0: rows longer than
-// that are read again for the gradient.
-template <int DT, int W, int NV>
-__global__ __launch_bounds__(LossTeam<W>::THREADS) void cross_entropy_kernel(LossArgs a) {
+// that are read again for the gradient. NT: streaming loads and stores, for bf16 rows of whole 16-byte
+// units (32 x 128 bf16 rows of 50257: 140 us without the hints, 129 with; 24 x 100 unaligned fp32 rows, whose
+// lines neighbouring lanes share: 165 and 197).
+// (Eight waves a SIMD: a CU then works on two rows of 16 waves, one loading while the other
+// computes.)
+template <int DT, int W, int NV, bool NT>
+__global__ __launch_bounds__(LossTeam<W>::THREADS, DT == DT_BF16 ? 8 : 4) void cross_entropy_kernel(LossArgs a) {
   __shared__ float red[2 * W];
   __shared__ float zt_s[LossTeam<W>::TEAMS];
   constexpr int LANES = W * WAVE, ES = Oct<DT>::ES;
@@ -178,20 +199,29 @@ __global__ __launch_bounds__(LossTeam<W>::THREADS) void cross_entropy_kernel(Los
   char* g = (char*)a.Gz + row * a.ldg * ES;
   if (y < 0 || y >= V) {
     if (lane == 0 && a.logp) a.logp[row] = 0.f;
-    zero_row<DT>(g, V, lane, LANES);
+    zero_row<DT, NT>(g, V, lane, LANES);
     return;
   }
   const float w = a.w[row];
   // In LDS before the first exchange: where the gradient replaces the logits
-  // (Gz = Z) another thread overwrites this one.
+  // (Gz = Z) this one is overwritten.
   if (lane == 0) zt_s[team] = logit_at<DT>(z, y);
+  if constexpr (W == 1) __builtin_amdgcn_wave_barrier();
   float top, sum = 0.f;
   Oct<DT> v[NV > 0 ? NV : 1];
+  // Makes the row opaque: unpacked values and exponentials that a later pass over it could
+  // use again would be kept, in several times its registers.
+  auto hide = [&]() __attribute__((always_inline)) {
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+#pragma unroll
+      for (int q = 0; q < (DT == DT_BF16 ? 1 : 2); ++q) asm volatile("" : "+v"(v[j].r[q]));
+  };
   if constexpr (NV > 0) {
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
       const int col = (lane + j * LANES) * 8;
-      v[j].load(z + (int64_t)col * ES, V - col, NEG_INF<DT>);
+      v[j].template load<NT>(z + (int64_t)col * ES, V - col, NEG_INF<DT>);
     }
     top = LOWEST;
 #pragma unroll
@@ -199,43 +229,46 @@ __global__ __launch_bounds__(LossTeam<W>::THREADS) void cross_entropy_kernel(Los
 #pragma unroll
       for (int e = 0; e < 8; ++e) top = fmaxf(top, v[j].at(e));
     top = team_max<W>(top, red);
+    hide();
     float none = 0.f;
 #pragma unroll
     for (int j = 0; j < NV; ++j)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) sum += exp_from(v[j].at(e), top);
+      for (int e = 0; e < 8; ++e) sum += exp_from<false>(v[j].at(e), top);
     team_sum2<W>(sum, none, red);
   } else {
-    row_sum<DT, W, 4>(z, V, lane, top, sum);
-    team_row<W>(top, sum, red);
+    row_sum<DT, W, 4, false>(z, V, lane, top, sum);
+    team_row<W, false>(top, sum, red);
   }
   if (lane == 0 && a.logp) a.logp[row] = (float)row_logp(zt_s[team], top, sum);
   if (w == 0.f || sum == 0.f) {
-    zero_row<DT>(g, V, lane, LANES);
+    zero_row<DT, NT>(g, V, lane, LANES);
     return;
   }
   const float f = w / sum;
+  hide();
   if constexpr (NV > 0) {
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
       const int col = (lane + j * LANES) * 8;
-      grad_octet<DT>(v[j], top, f, w, y - col);
-      v[j].store(g + (int64_t)col * ES, V - col);
+      grad_octet<DT>(v[j], top, f);
+      v[j].template store<NT>(g + (int64_t)col * ES, V - col);
     }
   } else {
     for (int col = lane * 8; col < V; col += LANES * 8) {
       Oct<DT> u;
-      u.load(z + (int64_t)col * ES, V - col, NEG_INF<DT>);
-      grad_octet<DT>(u, top, f, w, y - col);
-      u.store(g + (int64_t)col * ES, V - col);
+      u.template load<NT>(z + (int64_t)col * ES, V - col, NEG_INF<DT>);
+      grad_octet<DT>(u, top, f);
+      u.template store<NT>(g + (int64_t)col * ES, V - col);
     }
   }
+  if ((y >> 3) % LANES == lane) grad_target<DT>(g, y, zt_s[team], top, f, w);
 }
 
 // The preference loss's gradient from the rows' statistics and the pairs'
 // slopes: workgroup = (row, LG_OCTETS octets).
 constexpr int LG_U = 4, LG_THREADS = 256, LG_OCTETS = LG_U * LG_THREADS;
-template <int DT>
+template <int DT, bool NT>
 __global__ __launch_bounds__(LG_THREADS) void logit_grads_kernel(LossArgs a, uint32_t parts) {
   constexpr int ES = Oct<DT>::ES;
   const uint32_t r = blockIdx.x / parts;
@@ -254,22 +287,26 @@ __global__ __launch_bounds__(LG_THREADS) void logit_grads_kernel(LossArgs a, uin
 #pragma unroll
     for (int u = 0; u < LG_U; ++u) {
       const int col = (o0 + u * LG_THREADS) * 8;
-      v[0].store(g + (int64_t)col * ES, V - col);
+      v[0].template store<NT>(g + (int64_t)col * ES, V - col);
     }
     return;
   }
   const float f = w * st.scale;
+  // The target's logit, by the thread that replaces it.
+  const bool mine = (y >> 3) / LG_OCTETS == (int)(blockIdx.x - r * parts) && (y >> 3) % LG_THREADS == (int)threadIdx.x;
+  const float zt = mine ? logit_at<DT>(z, y) : 0.f;
 #pragma unroll
   for (int u = 0; u < LG_U; ++u) {
     const int col = (o0 + u * LG_THREADS) * 8;
-    v[u].load(z + (int64_t)col * ES, V - col, NEG_INF<DT>);
+    v[u].template load<NT>(z + (int64_t)col * ES, V - col, NEG_INF<DT>);
   }
 #pragma unroll
   for (int u = 0; u < LG_U; ++u) {
     const int col = (o0 + u * LG_THREADS) * 8;
-    grad_octet<DT>(v[u], st.top, f, w, y - col);
-    v[u].store(g + (int64_t)col * ES, V - col);
+    grad_octet<DT>(v[u], st.top, f);
+    v[u].template store<NT>(g + (int64_t)col * ES, V - col);
   }
+  if (mine) grad_target<DT>(g, y, zt, st.top, f, w);
 }
 
 // One workgroup per pair: the two sums of log-ratios, in double and in a fixed order.
@@ -315,58 +352,71 @@ __global__ __launch_bounds__(PF_THREADS) void preference_kernel(PreferenceArgs a
   a.slope[b] = (float)(beta * ((1.0 - eps) * down - eps * up));
 }
 
-// Threads of a row: a wave up to 2048 logits, 4 waves up to 8192, 16 above.
-hipError_t launch_token_logprobs(const LossArgs& a, int dt, hipStream_t s) {
-  const bool bf = dt == DT_BF16;
-  if (a.rows == 0) return hipSuccess;
-  const unsigned n = (unsigned)a.rows;
-  if (a.V <= 2048) {
-    const dim3 grid((n + 3) / 4), block(LossTeam<1>::THREADS);
-    if (bf) hipLaunchKernelGGL((token_logprobs_kernel<DT_BF16, 1>), grid, block, 0, s, a);
-    else hipLaunchKernelGGL((token_logprobs_kernel<DT_F32, 1>), grid, block, 0, s, a);
-  } else if (a.V <= 8192) {
-    const dim3 grid(n), block(LossTeam<4>::THREADS);
-    if (bf) hipLaunchKernelGGL((token_logprobs_kernel<DT_BF16, 4>), grid, block, 0, s, a);
-    else hipLaunchKernelGGL((token_logprobs_kernel<DT_F32, 4>), grid, block, 0, s, a);
-  } else {
-    const dim3 grid(n), block(LossTeam<16>::THREADS);
-    if (bf) hipLaunchKernelGGL((token_logprobs_kernel<DT_BF16, 16>), grid, block, 0, s, a);
-    else hipLaunchKernelGGL((token_logprobs_kernel<DT_F32, 16>), grid, block, 0, s, a);
-  }
+template <int DT, int W, int U>
+static hipError_t tl(const LossArgs& a, hipStream_t s) {
+  constexpr int TEAMS = LossTeam<W>::TEAMS;
+  const dim3 grid((unsigned)((a.rows + TEAMS - 1) / TEAMS)), block(LossTeam<W>::THREADS);
+  if (a.logp64) hipLaunchKernelGGL((token_logprobs_kernel<DT, W, U, true>), grid, block, 0, s, a);
+  else hipLaunchKernelGGL((token_logprobs_kernel<DT, W, U, false>), grid, block, 0, s, a);
   return hipGetLastError();
 }
 
-template <int DT, int W, int NV>
+// Threads of a row: a wave up to 2048 logits, 4 waves up to 8192. Above, 4 where there are
+// rows for every CU's every wave (rows then start and end at different times), 16 otherwise.
+template <int DT>
+static hipError_t tl_by_width(const LossArgs& a, hipStream_t s) {
+  if (a.V <= 2048) return tl<DT, 1, 4>(a, s);
+  if (a.V <= 8192 || a.rows >= 2048) return tl<DT, 4, 8>(a, s);
+  return tl<DT, 16, 8>(a, s);
+}
+
+hipError_t launch_token_logprobs(const LossArgs& a, int dt, hipStream_t s) {
+  if (a.rows == 0) return hipSuccess;
+  return dt == DT_BF16 ? tl_by_width<DT_BF16>(a, s) : tl_by_width<DT_F32>(a, s);
+}
+
+template <int DT, int W, int NV, bool NT>
 static hipError_t ce(const LossArgs& a, hipStream_t s) {
   const unsigned teams = LossTeam<W>::TEAMS;
-  hipLaunchKernelGGL((cross_entropy_kernel<DT, W, NV>),
+  hipLaunchKernelGGL((cross_entropy_kernel<DT, W, NV, NT>),
                      dim3((unsigned)((a.rows + teams - 1) / teams)), dim3(LossTeam<W>::THREADS), 0, s, a);
   return hipGetLastError();
 }
 
-template <int DT>
+template <int DT, bool NT>
 static hipError_t ce_by_width(const LossArgs& a, hipStream_t s) {
   const int octs = (a.V + 7) / 8;
-  if (octs <= 64) return ce<DT, 1, 1>(a, s);
-  if (octs <= 256) return ce<DT, 1, 4>(a, s);
-  if (octs <= 1024) return ce<DT, 4, 4>(a, s);
-  if (octs <= 4096) return ce<DT, 16, 4>(a, s);
-  if (octs <= 8192) return ce<DT, 16, 8>(a, s);
-  return ce<DT, 16, 0>(a, s);
+  if (octs <= 64) return ce<DT, 1, 1, NT>(a, s);
+  if (octs <= 256) return ce<DT, 1, 4, NT>(a, s);
+  if (octs <= 1024) return ce<DT, 4, 4, NT>(a, s);
+  if (octs <= 4096) return ce<DT, 16, 4, NT>(a, s);
+  if (octs <= 7168) return ce<DT, 16, 7, NT>(a, s);
+  return ce<DT, 16, 0, NT>(a, s);
+}
+
+// Whether every row of the logits and of the gradient starts on a 16-byte boundary.
+static bool aligned_rows(const LossArgs& a, int es) {
+  return (((uintptr_t)a.Gz | (uintptr_t)a.Z) & 15) == 0 && (a.ldg * es) % 16 == 0 && (a.ldz * es) % 16 == 0;
 }
 
 hipError_t launch_cross_entropy(const LossArgs& a, int dt, hipStream_t s) {
   if (a.rows == 0) return hipSuccess;
-  return dt == DT_BF16 ? ce_by_width<DT_BF16>(a, s) : ce_by_width<DT_F32>(a, s);
+  if (dt == DT_BF16) return aligned_rows(a, 2) ? ce_by_width<DT_BF16, true>(a, s) : ce_by_width<DT_BF16, false>(a, s);
+  return ce_by_width<DT_F32, false>(a, s);
+}
+
+template <int DT, bool NT>
+static hipError_t lg(const LossArgs& a, hipStream_t s) {
+  const uint32_t parts = (uint32_t)((((int64_t)a.V + 7) / 8 + LG_OCTETS - 1) / LG_OCTETS);
+  const dim3 grid((unsigned)(a.rows * parts)), block(LG_THREADS);
+  hipLaunchKernelGGL((logit_grads_kernel<DT, NT>), grid, block, 0, s, a, parts);
+  return hipGetLastError();
 }
 
 hipError_t launch_logit_grads(const LossArgs& a, int dt, hipStream_t s) {
   if (a.rows == 0) return hipSuccess;
-  const uint32_t parts = (uint32_t)((((int64_t)a.V + 7) / 8 + LG_OCTETS - 1) / LG_OCTETS);
-  const dim3 grid((unsigned)(a.rows * parts)), block(LG_THREADS);
-  if (dt == DT_BF16) hipLaunchKernelGGL((logit_grads_kernel<DT_BF16>), grid, block, 0, s, a, parts);
-  else hipLaunchKernelGGL((logit_grads_kernel<DT_F32>), grid, block, 0, s, a, parts);
-  return hipGetLastError();
+  if (dt == DT_BF16) return aligned_rows(a, 2) ? lg<DT_BF16, true>(a, s) : lg<DT_BF16, false>(a, s);
+  return lg<DT_F32, false>(a, s);
 }
 
 hipError_t launch_preference(const PreferenceArgs& a, int B, hipStream_t s) {

@@ -8,8 +8,16 @@ namespace dpg {
 constexpr float LOG2E = 1.4426950408889634f;
 
 typedef __attribute__((address_space(1))) u32x4_any global_u32x4_any_w;
+// NT: a hint that the line is not used again soon.
+template <bool NT>
 __device__ __forceinline__ void store16_any(char* p, const u32x4& v) {
-  *(global_u32x4_any_w*)(uintptr_t)p = v;
+  if constexpr (NT) __builtin_nontemporal_store(v, (global_u32x4_any_w*)(uintptr_t)p);
+  else *(global_u32x4_any_w*)(uintptr_t)p = v;
+}
+template <bool NT>
+__device__ __forceinline__ u32x4 load16_hint(const char* p) {
+  if constexpr (NT) return __builtin_nontemporal_load((global_u32x4_any*)(uintptr_t)p);
+  else return load16_any(p);
 }
 
 // An octet's bits as loaded: 16 bytes of bf16, 32 of fp32.
@@ -20,10 +28,11 @@ struct Oct {
 
   // Elements [0, n) at p (n may be past 8, or not positive: nothing is read); the
   // others are `fill`, as bits of the type twice in a dword (bf16) or once (fp32).
+  template <bool NT = false>
   __device__ __forceinline__ void load(const char* p, int64_t n, uint32_t fill = 0u) {
     if (n >= 8) {
-      r[0] = load16_any(p);
-      if constexpr (DT == DT_F32) r[1] = load16_any(p + 16);
+      r[0] = load16_hint<NT>(p);
+      if constexpr (DT == DT_F32) r[1] = load16_hint<NT>(p + 16);
       return;
     }
     if constexpr (DT == DT_BF16) {
@@ -59,10 +68,11 @@ struct Oct {
     }
   }
 
+  template <bool NT = false>
   __device__ __forceinline__ void store(char* p, int64_t n) const {
     if (n >= 8) {
-      store16_any(p, r[0]);
-      if constexpr (DT == DT_F32) store16_any(p + 16, r[1]);
+      store16_any<NT>(p, r[0]);
+      if constexpr (DT == DT_F32) store16_any<NT>(p + 16, r[1]);
       return;
     }
 #pragma unroll
@@ -76,17 +86,25 @@ struct Oct {
   }
 };
 
+// The sum over a row of 16 lanes, in each of them, by rotating adds (VALU, no LDS
+// permutes): lanes whose values meet add the same two in either order, so all hold the same bits.
+template <int N>
+__device__ __forceinline__ float row_rotate(float x) {
+  return __uint_as_float((uint32_t)__builtin_amdgcn_mov_dpp((int)__float_as_uint(x), 0x120 + N, 0xF, 0xF, true));
+}
+__device__ __forceinline__ float row16_sum(float x) {
+  x += row_rotate<8>(x);
+  x += row_rotate<4>(x);
+  x += row_rotate<2>(x);
+  return x + row_rotate<1>(x);
+}
+
 // Sums of two values over a team of W waves, in every thread: W = 1 a wave of
 // its own, otherwise the whole workgroup through `red` (2 W floats), in a fixed order.
 template <int W>
 __device__ __forceinline__ void team_sum2(float& a, float& b, float* red) {
-#pragma unroll
-  for (int off = 8; off >= 1; off >>= 1) {
-    a += __shfl_xor(a, off, WAVE);
-    b += __shfl_xor(b, off, WAVE);
-  }
-  a = xor32_sum(xor16_sum(a));
-  b = xor32_sum(xor16_sum(b));
+  a = xor32_sum(xor16_sum(row16_sum(a)));
+  b = xor32_sum(xor16_sum(row16_sum(b)));
   if constexpr (W > 1) {
     const int w = (int)threadIdx.x / WAVE;
     __syncthreads();   // the previous sums have been read

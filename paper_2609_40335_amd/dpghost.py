@@ -749,65 +749,73 @@ def dp_clipped_grad_sum_noised_store(layers: Sequence, outs: Sequence[torch.Tens
 
 
 
-def _same_device(stream, *named) -> None:
-    """Operands of one call: device tensors, all on the device the call is made on
-    (the stream's, or the current one)."""
-    at = torch.cuda.current_device() if stream is None else getattr(stream, "device_index",
-                                                                   torch.cuda.current_device())
-    if at != torch.cuda.current_device():
-        raise DPError("the stream belongs to another device than the current one")
+def _same_device(stream, *named) -> int:
+    """The raw stream of a call whose operands are device tensors on the device the call is
+    made on (the stream's, and the current one)."""
+    at = torch.cuda.current_device()
     for t, name in named:
-        if t is None:
-            continue
-        _dev(t, name)
-        if t.device.index != at:
+        if t is not None and t.get_device() != at:
+            _dev(t, name)
             raise DPError(f"{name} is on {t.device}, the call on cuda:{at}")
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(at)
+    if getattr(stream, "device_index", at) != at:
+        raise DPError("the stream belongs to another device than the current one")
+    return stream.cuda_stream
 
 
 def _f32(t, shape, name: str):
     """Pointer of a contiguous fp32 tensor of this shape (None: NULL)."""
     if t is None:
         return None
-    if t.dtype != torch.float32 or tuple(t.shape) != shape or not t.is_contiguous():
+    if t.dtype != torch.float32 or t.shape != shape or not t.is_contiguous():
         raise DPError(f"{name} must be contiguous fp32 {list(shape)}")
     return t.data_ptr()
 
 
-def _like(t, x, name: str, of: str):
-    """(pointer, row stride) of a tensor with x's shape and dtype."""
-    if t.dtype != x.dtype or t.shape != x.shape:
+def _tokens(t, name: str):
+    """(pointer, [B, T, w], row stride) of a token-major tensor, as _rows checks it."""
+    shape, st = t.shape, t.stride()
+    if len(shape) != 3 or st[2] != 1 or (shape[0] > 1 and st[0] != shape[1] * st[1]):
+        _rows(t, name)
+    return t.data_ptr(), shape, st[1]
+
+
+def _like(t, shape, dtype, name: str, of: str):
+    """(pointer, row stride) of a tensor of this shape and dtype."""
+    p, s, ld = _tokens(t, name)
+    if s != shape or t.dtype != dtype:
         raise DPError(f"{name} must have {of}'s shape and dtype")
-    p, _, _, _, ld = _rows(t, name)
     return p, ld
 
 
-def _params(d: int, **named):
+def _params(d: int, gain, bias=None):
     """Pointers and the common dtype of parameters of d elements (None: NULL)."""
-    dt, ptrs = DP_F32, []
-    given = [t for t in named.values() if t is not None]
-    for name, t in named.items():
+    dt, ptrs = None, []
+    for t in (gain, bias):
         if t is None:
             ptrs.append(None)
             continue
-        if tuple(t.shape) != (d,) or not t.is_contiguous() or t.dtype != given[0].dtype:
-            raise DPError(f"{name} must be contiguous [{d}], gain and bias of one dtype")
-        dt = _dtype(t)
+        if t.shape != (d,) or not t.is_contiguous() or (dt is not None and t.dtype != dt):
+            raise DPError(f"gain and bias must be contiguous [{d}] and of one dtype")
+        dt = t.dtype
         ptrs.append(t.data_ptr())
-    return ptrs, dt
+    return ptrs, DP_F32 if dt is None else _dtype(gain if gain is not None else bias)
 
 
 def dp_layernorm_forward(x, gain, bias, y, mean=None, rstd=None, eps: float = 1e-5,
                          stream=None) -> torch.Tensor:
     """y = gain * (x - mean) * rstd + bias per row of x [B, T, d]; gain, bias [d]
     (fp32 or bf16, or None); mean and rstd: fp32 [B, T] outputs for the backward pass."""
-    _same_device(stream, (x, "x"), (gain, "gain"), (bias, "bias"), (y, "y"), (mean, "mean"),
+    raw = _same_device(stream, (x, "x"), (gain, "gain"), (bias, "bias"), (y, "y"), (mean, "mean"),
                  (rstd, "rstd"))
-    px, B, T, d, ldx = _rows(x, "x")
-    py, ldy = _like(y, x, "y", "x")
-    (pg, pb), pdt = _params(d, gain=gain, bias=bias)
+    px, shape, ldx = _tokens(x, "x")
+    B, T, d = shape
+    py, ldy = _like(y, shape, x.dtype, "y", "x")
+    (pg, pb), pdt = _params(d, gain, bias)
     _check(lib().dp_layernorm_forward(px, ldx, pg, pb, pdt, B, T, d, _dtype(x), float(eps), py,
                                       ldy, _f32(mean, (B, T), "mean"), _f32(rstd, (B, T), "rstd"),
-                                      _stream(stream)), "dp_layernorm_forward")
+                                      raw), "dp_layernorm_forward")
     return y
 
 
@@ -818,12 +826,13 @@ def dp_layernorm_backward(gy, x, gain, mean, rstd, dx, dgain=None, dbias=None, n
     and dbias (fp32 [B, d], either may be None), and their squared norms into (accumulate:
     added to) norm2 (fp32 [B] or None). accumulate_dx adds onto dx."""
     L = lib()
-    _same_device(stream, (gy, "gy"), (x, "x"), (gain, "gain"), (mean, "mean"), (rstd, "rstd"),
+    raw = _same_device(stream, (gy, "gy"), (x, "x"), (gain, "gain"), (mean, "mean"), (rstd, "rstd"),
                  (dx, "dx"), (dgain, "dgain"), (dbias, "dbias"), (norm2, "norm2"))
-    pg, B, T, d, ldg = _rows(gy, "gy")
-    px, ldx = _like(x, gy, "x", "gy")
-    pd, ldd = (None, 0) if dx is None else _like(dx, gy, "dx", "gy")
-    (pw,), pdt = _params(d, gain=gain)
+    pg, shape, ldg = _tokens(gy, "gy")
+    B, T, d = shape
+    px, ldx = _like(x, shape, gy.dtype, "x", "gy")
+    pd, ldd = (None, 0) if dx is None else _like(dx, shape, gy.dtype, "dx", "gy")
+    (pw, _), pdt = _params(d, gain)
     ws, nbytes = None, 0
     if dgain is not None or dbias is not None:
         nbytes = L.dp_layernorm_backward_workspace(B, T, d)
@@ -833,36 +842,38 @@ def dp_layernorm_backward(gy, x, gain, mean, rstd, dx, dgain=None, dbias=None, n
                                    int(accumulate_dx), _f32(dgain, (B, d), "dgain"),
                                    _f32(dbias, (B, d), "dbias"), _f32(norm2, (B,), "norm2"),
                                    int(accumulate), None if ws is None else ws.data_ptr(), nbytes,
-                                   _stream(stream)), "dp_layernorm_backward")
+                                   raw), "dp_layernorm_backward")
 
 
 def _logits(Z, targets):
-    pz, B, T, V, ldz = _rows(Z, "Z")
-    if targets.dtype != torch.int32 or tuple(targets.shape) != (B, T) or not targets.is_contiguous():
+    pz, shape, ldz = _tokens(Z, "Z")
+    if targets.dtype != torch.int32 or targets.shape != shape[:2] or not targets.is_contiguous():
         raise DPError("targets must be contiguous int32 [B, T]")
-    return pz, B, T, V, ldz
+    return pz, shape, ldz
 
 
 def dp_token_logprobs(Z, targets, logp, lse=None, stream=None) -> torch.Tensor:
     """logp [B, T] = log softmax(Z)[target] (0 where the target is outside [0, V)),
     lse [B, T] the logarithm of the row's sum of exponentials."""
-    _same_device(stream, (Z, "Z"), (targets, "targets"), (logp, "logp"), (lse, "lse"))
-    pz, B, T, V, ldz = _logits(Z, targets)
+    raw = _same_device(stream, (Z, "Z"), (targets, "targets"), (logp, "logp"), (lse, "lse"))
+    pz, shape, ldz = _logits(Z, targets)
+    B, T, V = shape
     _check(lib().dp_token_logprobs(pz, ldz, targets.data_ptr(), B, T, V, _dtype(Z),
                                    _f32(logp, (B, T), "logp"), _f32(lse, (B, T), "lse"),
-                                   _stream(stream)), "dp_token_logprobs")
+                                   raw), "dp_token_logprobs")
     return logp
 
 
 def dp_cross_entropy(Z, targets, w, logp, Gz, stream=None) -> torch.Tensor:
     """Gz = w (softmax(Z) - onehot(targets)), the gradient of sum_t w (-logp); logp
     (fp32 [B, T] or None) as dp_token_logprobs. Gz may be Z."""
-    _same_device(stream, (Z, "Z"), (targets, "targets"), (w, "w"), (logp, "logp"), (Gz, "Gz"))
-    pz, B, T, V, ldz = _logits(Z, targets)
-    pg, ldg = _like(Gz, Z, "Gz", "Z")
+    raw = _same_device(stream, (Z, "Z"), (targets, "targets"), (w, "w"), (logp, "logp"), (Gz, "Gz"))
+    pz, shape, ldz = _logits(Z, targets)
+    B, T, V = shape
+    pg, ldg = _like(Gz, shape, Z.dtype, "Gz", "Z")
     _check(lib().dp_cross_entropy(pz, ldz, targets.data_ptr(), _f32(w, (B, T), "w"), B, T, V,
                                   _dtype(Z), _f32(logp, (B, T), "logp"), pg, ldg,
-                                  _stream(stream)), "dp_cross_entropy")
+                                  raw), "dp_cross_entropy")
     return Gz
 
 
@@ -873,10 +884,11 @@ def dp_preference_loss(Z, targets, split: int, ref_logp, beta: float, loss, rewa
     reference model's log-probabilities ref_logp [B, T] (or None); rewards [B, 2], logp
     [B, T] and Gz = d loss / d Z are optional. Gz may be Z."""
     L = lib()
-    _same_device(stream, (Z, "Z"), (targets, "targets"), (ref_logp, "ref_logp"), (loss, "loss"),
+    raw = _same_device(stream, (Z, "Z"), (targets, "targets"), (ref_logp, "ref_logp"), (loss, "loss"),
                  (rewards, "rewards"), (logp, "logp"), (Gz, "Gz"))
-    pz, B, T, V, ldz = _logits(Z, targets)
-    pg, ldg = (None, 0) if Gz is None else _like(Gz, Z, "Gz", "Z")
+    pz, shape, ldz = _logits(Z, targets)
+    B, T, V = shape
+    pg, ldg = (None, 0) if Gz is None else _like(Gz, shape, Z.dtype, "Gz", "Z")
     nbytes = L.dp_preference_loss_workspace(B, T)
     ws = _ws(nbytes, Z.device, stream)
     _check(L.dp_preference_loss(pz, ldz, targets.data_ptr(), int(split),
@@ -884,7 +896,7 @@ def dp_preference_loss(Z, targets, split: int, ref_logp, beta: float, loss, rewa
                                 float(label_smoothing), B, T, V, _dtype(Z),
                                 _f32(loss, (B,), "loss"), _f32(rewards, (B, 2), "rewards"),
                                 _f32(logp, (B, T), "logp"), pg, ldg, ws.data_ptr(), nbytes,
-                                _stream(stream)), "dp_preference_loss")
+                                raw), "dp_preference_loss")
     return loss
 
 
@@ -906,7 +918,7 @@ def dp_orthogonalize_grouped(grads: Sequence[torch.Tensor], outs: Sequence[torch
     scales = list(scale) if isinstance(scale, (list, tuple)) else [scale] * n
     if len(scales) != n:
         raise DPError("one scale per matrix")
-    _same_device(stream, *((g, f"grads[{l}]") for l, g in enumerate(grads)),
+    raw = _same_device(stream, *((g, f"grads[{l}]") for l, g in enumerate(grads)),
                  *((o, f"outs[{l}]") for l, o in enumerate(outs)))
     dt, odt = grads[0].dtype, outs[0].dtype
     arr = (dp_matrix_t * n)()
@@ -928,7 +940,7 @@ def dp_orthogonalize_grouped(grads: Sequence[torch.Tensor], outs: Sequence[torch
     nbytes = L.dp_orthogonalize_workspace(arr, n, _odt)
     ws = _ws(nbytes, grads[0].device, stream)
     _check(L.dp_orthogonalize_grouped(arr, n, _dt, _odt, cf, int(steps), float(eps),
-                                      int(accumulate), ws.data_ptr(), nbytes, _stream(stream)),
+                                      int(accumulate), ws.data_ptr(), nbytes, raw),
            "dp_orthogonalize_grouped")
 
 

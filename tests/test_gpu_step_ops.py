@@ -247,7 +247,12 @@ def test_masked_and_extreme_logits(dp, dt, V):
     lse = torch.empty(1, 9, device="cuda")
     l2 = torch.empty_like(logp)
     dp.dp_token_logprobs(zd, y.cuda(), l2, lse=lse)
-    assert torch.equal(torch.nan_to_num(logp, nan=3.0), torch.nan_to_num(l2, nan=3.0))
+    # Both are within their bound of the same value, so within twice that of one another.
+    _, _, es = F.token_logprobs(z.double().numpy()[:, [0, 1, 3, 4]], y.numpy()[:, [0, 1, 3, 4]])
+    a, b = _host(logp)[0], _host(l2)[0]
+    assert (np.isnan(a) == np.isnan(b)).all() and (np.isinf(a) == np.isinf(b)).all()
+    for k, r in enumerate((0, 1, 3, 4)):
+        assert abs(a[r] - b[r]) <= 2 * (es[0, k] + F.U * abs(a[r])), r
     lp, gz = _host(logp)[0], _host(g)[0]
     assert lp[0] == 0 and not gz[0].any()
     assert lp[2] == -np.inf and float(lse[0, 2]) == -np.inf and not gz[2].any()

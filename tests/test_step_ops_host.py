@@ -113,11 +113,11 @@ def test_binding_refuses_host_tensors_and_wrong_shapes(monkeypatch):
     with pytest.raises(D.DPError, match="fp32"):
         D._f32(torch.zeros(2, 3, dtype=torch.float64), (2, 3), "mean")
     with pytest.raises(D.DPError, match="shape and dtype"):
-        D._like(torch.zeros(2, 3, 9), x, "y", "x")
+        D._like(torch.zeros(2, 3, 9), x.shape, x.dtype, "y", "x")
     with pytest.raises(D.DPError, match="gain"):
-        D._params(8, gain=torch.zeros(7))
+        D._params(8, torch.zeros(7))
     with pytest.raises(D.DPError, match="one dtype"):
-        D._params(8, gain=torch.zeros(8), bias=torch.zeros(8, dtype=torch.bfloat16))
+        D._params(8, torch.zeros(8), torch.zeros(8, dtype=torch.bfloat16))
 
 
 def _autograd_preference(z, targets, split, ref, beta, eps):
