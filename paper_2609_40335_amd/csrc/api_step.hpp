@@ -60,15 +60,19 @@ dp_status_t check_in_place(const void* Z, int64_t ldz, const void* Gz, int64_t l
 }
 
 inline int ns_padded(int x) { return (int)ceil_div(x, dpg::NS_TILE) * dpg::NS_TILE; }
-inline int ns_planes(dp_dtype_t out_dt) { return out_dt == DP_BF16 ? 1 : 2; }
+// Planes of a matrix's operands. Few rows average few roundings: of 16 x 16 a bf16 result's
+// products alone are 2.0e-3 off with one plane, of 64 x 64 1.5e-3, from 200 x 200 on 1.2e-3.
+inline int ns_planes(const dp_matrix_t& m, dp_dtype_t out_dt) {
+  return out_dt == DP_BF16 && std::min(m.rows, m.cols) > 64 ? 1 : 2;
+}
 
-// The launches of a group: up to NS_MAX_MATS matrices each, from *next on; the small ones
-// (dpg::ns_small) and the others apart.
-dpg::NsArgs ns_batch(const dp_matrix_t* m, int n, int pl, bool small, int* next) {
+// The launches of a group: up to NS_MAX_MATS matrices each, from *next on; those of one and of
+// two planes, and the small ones (dpg::ns_small), apart.
+dpg::NsArgs ns_batch(const dp_matrix_t* m, int n, dp_dtype_t out_dt, int pl, bool small, int* next) {
   dpg::NsArgs a{};
   for (; *next < n && a.n < dpg::NS_MAX_MATS; ++*next) {
     const dp_matrix_t& x = m[*next];
-    if (dpg::ns_small(x.rows, x.cols, pl) != small) continue;
+    if (ns_planes(x, out_dt) != pl || dpg::ns_small(x.rows, x.cols, pl) != small) continue;
     dpg::NsMat& M = a.M[a.n++];
     M.G = x.G; M.out = x.out; M.ldg = x.ldg; M.ldo = x.ldo;
     M.rows = x.rows; M.cols = x.cols; M.scale = x.scale;
@@ -104,10 +108,11 @@ dp_status_t check_matrices(const dp_matrix_t* m, int n, dp_dtype_t in_dt, dp_dty
       return fail(DP_EUNSUPPORTED, "matrix %d: 2^30 elements or more", l);
   }
   *bytes = 0;
-  for (int next = 0; next < n;) {
-    const dpg::NsArgs a = ns_batch(m, n, ns_planes(out_dt), false, &next);
-    if (a.n) *bytes = std::max(*bytes, ns_batch_bytes(a, ns_planes(out_dt)));
-  }
+  for (int pl = 1; pl <= 2; ++pl)
+    for (int next = 0; next < n;) {
+      const dpg::NsArgs a = ns_batch(m, n, out_dt, pl, false, &next);
+      if (a.n) *bytes = std::max(*bytes, ns_batch_bytes(a, pl));
+    }
   return DP_OK;
 }
 
@@ -286,29 +291,27 @@ dp_status_t dp_orthogonalize_grouped(const dp_matrix_t* matrices, int n, dp_dtyp
   if (need && (!workspace || workspace_bytes < need))
     return fail(DP_EINVAL, "workspace of %zu bytes needed", need);
   if (need && !aligned16(workspace)) return fail(DP_EINVAL, "workspace must be 16-byte aligned");
-  const int pl = ns_planes(out_dt);
-  for (int next = 0; next < n;) {
-    dpg::NsArgs a = ns_batch(matrices, n, pl, true, &next);
-    if (a.n == 0) break;
-    a.out_dt = kdt(out_dt); a.accumulate = accumulate ? 1 : 0; a.eps = eps;
-    st = hip_status(dpg::launch_orthogonalize_small(a, kdt(in_dt), pl, coef, steps, as_stream(stream)),
-                    "orthogonalize launch");
-    if (st != DP_OK) return st;
-  }
-  for (int next = 0; next < n;) {
-    dpg::NsArgs a = ns_batch(matrices, n, pl, false, &next);
-    if (a.n == 0) break;
-    a.out_dt = kdt(out_dt); a.accumulate = accumulate ? 1 : 0; a.eps = eps;
-    char* ws = static_cast<char*>(workspace);
-    for (int l = 0; l < a.n; ++l) {
-      a.M[l].ws = ws;
-      ws += align_up(dpg::ns_bytes(a.M[l].mp, a.M[l].np, pl));
-    }
-    a.part = reinterpret_cast<float*>(ws);
-    st = hip_status(dpg::launch_orthogonalize(a, kdt(in_dt), pl, coef, steps, as_stream(stream)),
-                    "orthogonalize launch");
-    if (st != DP_OK) return st;
-  }
+  for (int pl = 1; pl <= 2; ++pl)
+    for (int big = 0; big <= 1; ++big)
+      for (int next = 0; next < n;) {
+        dpg::NsArgs a = ns_batch(matrices, n, out_dt, pl, !big, &next);
+        if (a.n == 0) break;
+        a.out_dt = kdt(out_dt); a.accumulate = accumulate ? 1 : 0; a.eps = eps;
+        hipError_t e;
+        if (big) {
+          char* ws = static_cast<char*>(workspace);
+          for (int l = 0; l < a.n; ++l) {
+            a.M[l].ws = ws;
+            ws += align_up(dpg::ns_bytes(a.M[l].mp, a.M[l].np, pl));
+          }
+          a.part = reinterpret_cast<float*>(ws);
+          e = dpg::launch_orthogonalize(a, kdt(in_dt), pl, coef, steps, as_stream(stream));
+        } else {
+          e = dpg::launch_orthogonalize_small(a, kdt(in_dt), pl, coef, steps, as_stream(stream));
+        }
+        st = hip_status(e, "orthogonalize launch");
+        if (st != DP_OK) return st;
+      }
   return DP_OK;
 }
 

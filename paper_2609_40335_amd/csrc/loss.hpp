@@ -34,15 +34,13 @@ constexpr float LOWEST = -FLT_MAX;   // running maximum of no logits (finite: -i
 template <int DT>
 constexpr uint32_t NEG_INF = DT == DT_BF16 ? 0xFF80FF80u : 0xFF800000u;
 
-// EXACT: log2 e in two parts. As one fp32 number it is 1.3e-8 of itself off, the same way in
-// every row, which a sum of hundreds of log-probabilities shows.
-template <bool EXACT>
-__device__ __forceinline__ float exp_from(float z, float top) {
-  constexpr float LO = (float)(1.4426950408889634 - (double)LOG2E);
-  static_assert(LO > 0.f, "-inf LO is -inf");
-  const float d = z - top;
-  return __builtin_amdgcn_exp2f(EXACT ? fmaf(d, LO, d * LOG2E) : d * LOG2E);
-}
+// exp(d) for d <= 0. log2 e as one fp32 number is LOG2E_LOST off (1.3e-8 of itself), so that
+// every exp(d) is off by d LOST of itself, the same way in every row: 6e-8 of a sum of
+// exponentials, which a sum of hundreds of log-probabilities shows. Such sums (EXACT) add
+// up d exp(d) as well and put the first order back. (As a second term of the exponent it would be
+// rounded away.)
+constexpr double LOST = 1.4426950408889634 / (double)LOG2E - 1.0;
+__device__ __forceinline__ float exp_of(float d) { return __builtin_amdgcn_exp2f(d * LOG2E); }
 
 __device__ __forceinline__ float wave_max(float v) {
 #pragma unroll
@@ -72,15 +70,72 @@ struct LossTeam {
   static constexpr int TEAMS = W == 1 ? 4 : 1;
 };
 
-// Running maximum and sum of exponentials of the lane's logits: octets `lane`,
-// `lane` + LANES, ... of the row, U of them in flight. EXACT rows are read a second time soon, others take
-// streaming loads in bf16 (24 x 128 rows of 50257: 57 us without the hint, 55 with; in fp32, where a lane's octet is two
-// loads of the same line, 83 and 101).
+// A running sum of exponentials from `top`. EXACT: in double, with that of d exp(d): a
+// factor from one maximum to the next that is rounded to fp32 is off the same way wherever
+// the same two maxima meet, and bf16 logits have few of them.
+template <bool EXACT>
+struct RunningSum {
+  float top = LOWEST, sum = 0.f;
+  __device__ __forceinline__ void move(float m) {
+    sum *= exp_of(top - m);
+    top = m;
+  }
+  __device__ __forceinline__ void add(float s, float) { sum += s; }
+  __device__ __forceinline__ double total() const { return (double)sum; }
+  template <int W>
+  __device__ __forceinline__ void meet(double* red) {   // of a team
+    float none = 0.f;
+    move(team_max<W>(top, (float*)red));
+    team_sum2<W>(sum, none, (float*)red);
+  }
+};
+template <>
+struct RunningSum<true> {
+  float top = LOWEST;
+  double sum = 0.0, slope = 0.0;
+  __device__ __forceinline__ void move(float m) {
+    if (m != top) {
+      const double x = exp((double)top - (double)m);
+      sum *= x;
+      slope *= x;   // d up to the maximum that its exponential was taken from: x is exact
+      top = m;
+    }
+  }
+  __device__ __forceinline__ void add(float s, float t) {
+    sum += (double)s;
+    slope += (double)t;
+  }
+  __device__ __forceinline__ double total() const { return fma(LOST, slope, sum); }
+  template <int W>
+  __device__ __forceinline__ void meet(double* red) {
+    move(team_max<W>(top, (float*)red));
+    sum = wave_sum_d(sum);
+    slope = wave_sum_d(slope);
+    if constexpr (W > 1) {
+      const int w = (int)threadIdx.x / WAVE;
+      __syncthreads();
+      if (threadIdx.x % WAVE == 0) {
+        red[2 * w] = sum;
+        red[2 * w + 1] = slope;
+      }
+      __syncthreads();
+      sum = slope = 0.0;
+      for (int i = 0; i < W; ++i) {
+        sum += red[2 * i];
+        slope += red[2 * i + 1];
+      }
+    }
+  }
+};
+
+// That of the lane's logits: octets `lane`, `lane` + LANES, ... of the row, U of them in
+// flight. EXACT rows are read a second time soon, others take streaming loads in bf16 (24 x 128
+// rows of 50257: 57 us without the hint, 55 with; in fp32, where a lane's octet is two loads of the
+// same line, 83 and 101).
 template <int DT, int W, int U, bool EXACT>
-__device__ __forceinline__ void row_sum(const char* z, int V, int lane, float& top, float& sum) {
+__device__ __forceinline__ RunningSum<EXACT> row_sum(const char* z, int V, int lane) {
   constexpr int LANES = W * WAVE;
-  top = LOWEST;
-  sum = 0.f;
+  RunningSum<EXACT> s;
   for (int o = lane; o * 8 < V; o += U * LANES) {
     Oct<DT> v[U];
 #pragma unroll
@@ -88,32 +143,28 @@ __device__ __forceinline__ void row_sum(const char* z, int V, int lane, float& t
       const int col = (o + u * LANES) * 8;
       v[u].template load<!EXACT && DT == DT_BF16>(z + (int64_t)col * Oct<DT>::ES, V - col, NEG_INF<DT>);
     }
-    float m = top;
+    float m = s.top;
 #pragma unroll
     for (int u = 0; u < U; ++u)
 #pragma unroll
       for (int e = 0; e < 8; ++e) m = fmaxf(m, v[u].at(e));
-    sum *= exp_from<EXACT>(top, m);
+    s.move(m);
+    float part = 0.f, slope = 0.f;
 #pragma unroll
     for (int u = 0; u < U; ++u)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) sum += exp_from<EXACT>(v[u].at(e), m);
-    top = m;
+      for (int e = 0; e < 8; ++e) {
+        const float d = v[u].at(e) - m, x = exp_of(d);
+        part += x;
+        if constexpr (EXACT) slope = fmaf(fmaxf(d, -200.f), x, slope);   // x is 0 below
+      }
+    s.add(part, slope);
   }
+  return s;
 }
 
-// The team's: every thread gets the row's maximum and sum.
-template <int W, bool EXACT>
-__device__ __forceinline__ void team_row(float& top, float& sum, float* red) {
-  const float m = team_max<W>(top, red);
-  float s = sum * exp_from<EXACT>(top, m), none = 0.f;
-  team_sum2<W>(s, none, red);
-  top = m;
-  sum = s;
-}
-
-__device__ __forceinline__ double row_logp(float zt, float top, float sum) {
-  return sum == 0.f ? -__builtin_inf() : (double)zt - (double)top - log((double)sum);
+__device__ __forceinline__ double row_logp(float zt, float top, double sum) {
+  return sum == 0.0 ? -__builtin_inf() : (double)zt - (double)top - log(sum);
 }
 
 template <int DT>
@@ -124,7 +175,7 @@ __device__ __forceinline__ float logit_at(const char* z, int col) {
 
 template <int DT, int W, int U, bool EXACT>
 __global__ __launch_bounds__(LossTeam<W>::THREADS) void token_logprobs_kernel(LossArgs a) {
-  __shared__ float red[2 * W];
+  __shared__ double red[2 * W];
   const int lane = (int)threadIdx.x % (W * WAVE), team = (int)threadIdx.x / (W * WAVE);
   const int64_t r = (int64_t)blockIdx.x * LossTeam<W>::TEAMS + team;
   if (r >= a.rows) return;
@@ -141,15 +192,14 @@ __global__ __launch_bounds__(LossTeam<W>::THREADS) void token_logprobs_kernel(Lo
   }
   const char* z = (const char*)a.Z + row * a.ldz * Oct<DT>::ES;
   const float zt = logit_at<DT>(z, y);
-  float top, sum;
-  row_sum<DT, W, U, EXACT>(z, a.V, lane, top, sum);
-  team_row<W, EXACT>(top, sum, red);
+  RunningSum<EXACT> s = row_sum<DT, W, U, EXACT>(z, a.V, lane);
+  s.template meet<W>(red);
   if (lane == 0) {
-    const double logp = row_logp(zt, top, sum);
+    const double total = s.total(), logp = row_logp(zt, s.top, total);
     if (a.logp) a.logp[row] = (float)logp;
-    if (a.lse) a.lse[row] = sum == 0.f ? -__builtin_inff() : (float)((double)top + log((double)sum));
+    if (a.lse) a.lse[row] = total == 0.0 ? -__builtin_inff() : (float)((double)s.top + log(total));
     if (a.logp64) a.logp64[row] = logp;
-    if (a.stat) a.stat[row] = RowStat{top, sum == 0.f ? 0.f : 1.f / sum};
+    if (a.stat) a.stat[row] = RowStat{s.top, total == 0.0 ? 0.f : (float)(1.0 / total)};
   }
 }
 
@@ -159,12 +209,12 @@ template <int DT>
 __device__ __forceinline__ void grad_octet(Oct<DT>& v, float top, float f) {
   float o[8];
 #pragma unroll
-  for (int e = 0; e < 8; ++e) o[e] = exp_from<false>(v.at(e), top) * f;
+  for (int e = 0; e < 8; ++e) o[e] = exp_of(v.at(e) - top) * f;
   v.set(o);
 }
 template <int DT>
 __device__ __forceinline__ void grad_target(char* g, int y, float zt, float top, float f, float w) {
-  const float v = fmaf(exp_from<false>(zt, top), f, -w);
+  const float v = fmaf(exp_of(zt - top), f, -w);
   if constexpr (DT == DT_BF16)
     ((uint16_t*)g)[y] = (uint16_t)__builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{v, v}, bf16x2));
   else
@@ -188,7 +238,7 @@ __device__ __forceinline__ void zero_row(char* g, int V, int lane, int lanes) {
 // computes.)
 template <int DT, int W, int NV, bool NT>
 __global__ __launch_bounds__(LossTeam<W>::THREADS, DT == DT_BF16 ? 8 : 4) void cross_entropy_kernel(LossArgs a) {
-  __shared__ float red[2 * W];
+  __shared__ double red[2 * W];
   __shared__ float zt_s[LossTeam<W>::TEAMS];
   constexpr int LANES = W * WAVE, ES = Oct<DT>::ES;
   const int lane = (int)threadIdx.x % LANES, team = (int)threadIdx.x / LANES;
@@ -228,17 +278,19 @@ __global__ __launch_bounds__(LossTeam<W>::THREADS, DT == DT_BF16 ? 8 : 4) void c
     for (int j = 0; j < NV; ++j)
 #pragma unroll
       for (int e = 0; e < 8; ++e) top = fmaxf(top, v[j].at(e));
-    top = team_max<W>(top, red);
+    top = team_max<W>(top, (float*)red);
     hide();
     float none = 0.f;
 #pragma unroll
     for (int j = 0; j < NV; ++j)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) sum += exp_from<false>(v[j].at(e), top);
-    team_sum2<W>(sum, none, red);
+      for (int e = 0; e < 8; ++e) sum += exp_of(v[j].at(e) - top);
+    team_sum2<W>(sum, none, (float*)red);
   } else {
-    row_sum<DT, W, 4, false>(z, V, lane, top, sum);
-    team_row<W, false>(top, sum, red);
+    RunningSum<false> all = row_sum<DT, W, 4, false>(z, V, lane);
+    all.meet<W>(red);
+    top = all.top;
+    sum = all.sum;
   }
   if (lane == 0 && a.logp) a.logp[row] = (float)row_logp(zt_s[team], top, sum);
   if (w == 0.f || sum == 0.f) {
