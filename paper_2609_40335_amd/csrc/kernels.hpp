@@ -577,35 +577,50 @@ DPG_HD inline size_t ns_bytes(int mp, int np, int pl) {
   return ns_offset(mp, np, NS_P, 0, pl) + (size_t)pl * mp * mp * 2;
 }
 #undef DPG_HD
-// Ranges of k that a symmetric product's tiles are cut into. One workgroup keeps a CU's
-// matrix cores as busy as two do (a second one only fills the first's gaps), so a launch
-// runs 256 items at a time, each for about its k and 600 more, US_K us per k; joining the
-// ranges is another launch. Cut where a launch fills at most half a round and that pays. (1601
-// x 6397, two planes, us: X X^T 103 whole and 67 + 9 in 5 ranges, A^2 35 and 20 + 8 in 2; 2048 x
-// 8192, one plane, 136 tiles: 75 whole, 58 + 13 in 3.)
+// How a product is launched: 64 x 64 tiles (small), or large ones, those of a symmetric
+// product perhaps in ks ranges of k.
+//
+// One workgroup with a large tile keeps a CU's matrix cores as busy as two do (a second one
+// only fills the first's gaps), so a launch runs 256 items at a time, each for about its k and
+// 600 more, US_K us per k; joining ranges is another launch. Ranges are cut where a launch fills
+// at most half a round and that pays. (1601 x 6397, two planes, us: X X^T 103 whole and 67 + 9 in
+// 5 ranges, A^2 35 and 20 + 8 in 2; 2048 x 8192, one plane, 136 tiles: 75 whole, 58 + 13 in 3.)
+// Small tiles cost more LDS reads and loads per product, but a launch of few of them ends
+// sooner: 6 us and US_K_SMALL per k, 512 at a time with one plane and 256 with two (their rings). All five
+// steps, us, large and small: 600 x 600 fp32 results 251, 153; bf16 188, 116; 1536 x 1536 bf16 350, 269;
+// and 100 x 3000 fp32, X X^T alone small: 144, 210; 1536 x 1536 fp32, updates alone: 419, 451.
+struct NsPlan {
+  int ks;
+  bool small;
+};
 constexpr double NS_JOIN_US = 8.0;
-inline int ns_split(const NsArgs& a, int kind, int pl) {
-  const double us_k = pl == 1 ? 0.008 : 0.0136;
-  int64_t tiles = 0, k_most = 0, k_least = 1 << 30;
+inline NsPlan ns_plan(const NsArgs& a, int kind, int pl) {
+  const bool sym = kind == NS_GRAM || kind == NS_POLY;
+  const double us_k = pl == 2 ? 0.0136 : sym ? 0.008 : 0.010, us_k_small = pl == 2 ? 0.0067 : 0.0045;
+  const int64_t at_once = pl == 2 ? 256 : 512;
+  int64_t tiles = 0, few = 0, k_most = 0, k_least = 1 << 30;   // few: large tiles
   for (int l = 0; l < a.n; ++l) {
-    const int64_t t = (a.M[l].mp + NS_TILE - 1) / NS_TILE, k = kind == NS_GRAM ? a.M[l].np : a.M[l].mp;
-    tiles += t * (t + 1) / 2;
+    const int64_t m = a.M[l].mp / 64, n = a.M[l].np / 64, k = kind == NS_GRAM ? a.M[l].np : a.M[l].mp;
+    tiles += sym ? m * (m + 1) / 2 : m * n;
+    few += sym ? m / 2 * (m / 2 + 1) / 2 : m / 2 * ((n / 2 + 2 - pl) / (3 - pl));
     k_most = k > k_most ? k : k_most;
     k_least = k < k_least ? k : k_least;
   }
-  if (tiles > 128) return 1;
-  int best = 1;
-  double best_us = (double)(k_most + 600) * us_k;
-  for (int ks = 2; ks <= 16 && ks * 128 <= k_least; ++ks) {
-    const double us = (double)((tiles * ks + 255) / 256) * ((double)k_most / ks + 600) * us_k + NS_JOIN_US;
-    if (us < 0.95 * best_us) { best_us = us; best = ks; }
-  }
+  NsPlan best{1, false};
+  double best_us = (double)((few + 255) / 256) * (double)(k_most + 600) * us_k;
+  if (sym && few <= 128)
+    for (int ks = 2; ks <= 16 && ks * 128 <= k_least; ++ks) {
+      const double us = (double)((few * ks + 255) / 256) * ((double)k_most / ks + 600) * us_k + NS_JOIN_US;
+      if (us < 0.95 * best_us) { best_us = us; best.ks = ks; }
+    }
+  const int64_t rounds = (tiles + at_once - 1) / at_once;
+  if (rounds <= 2 && 6.0 + (double)rounds * (double)k_most * us_k_small < 1.1 * best_us) best = NsPlan{1, true};
   return best;
 }
 inline size_t ns_part_bytes(const NsArgs& a, int pl) {
   size_t most = 0;
   for (int kind = NS_GRAM; kind <= NS_POLY; ++kind) {
-    const int ks = ns_split(a, kind, pl);
+    const int ks = ns_plan(a, kind, pl).ks;
     if (ks == 1) continue;
     size_t tiles = 0;
     for (int l = 0; l < a.n; ++l) {

@@ -300,7 +300,8 @@ struct NsShape {
   static constexpr int STAGE = PL * 64 * (FM + FN) * NS_BK * 2;
   static constexpr int GROUPS = 3 * STAGE * 2 <= 160 * 1024 && FM * FN <= 8 ? 2 : 1;
   static constexpr int FIT = 160 * 1024 / GROUPS / STAGE;
-  static constexpr int RING = FIT > 4 ? 4 : FIT;
+  static constexpr int DEEP = FM * FN == 1 ? 8 : 4;   // small tiles: latency is all there is
+  static constexpr int RING = FIT > DEEP ? DEEP : FIT;
   static_assert(RING >= 3, "a stage is loaded two ahead");
 };
 
@@ -826,7 +827,9 @@ static hipError_t ns_launch(NsArgs& a, const NsBins& bins, hipStream_t s) {
 
 template <int PL, int KIND>
 static hipError_t ns_symmetric(NsArgs& a, const NsBins& bins, hipStream_t s) {
-  a.ks = ns_split(a, KIND, PL);
+  const NsPlan plan = ns_plan(a, KIND, PL);
+  a.ks = plan.ks;
+  if (plan.small) return ns_launch<PL, KIND, 1, 1, false>(a, bins, s);
   if (a.ks == 1) return ns_launch<PL, KIND, 2, 2, false>(a, bins, s);
   const hipError_t e = ns_launch<PL, KIND, 2, 2, true>(a, bins, s);
   if (e != hipSuccess) return e;
@@ -839,7 +842,7 @@ static hipError_t ns_symmetric(NsArgs& a, const NsBins& bins, hipStream_t s) {
   return hipGetLastError();
 }
 
-// Tiles: 128 x 128 for the symmetric products, whose launches have few; for updates
+// Large tiles: 128 x 128 for the symmetric products, whose launches have few; for updates
 // 128 x 256 with one plane (fewer LDS reads per product: 171 us for GPT-2's blocks, 197 with 128 x
 // 128), 128 x 128 with two (105 us for 1601 x 6397, 116 with 256 x 128, which leave no
 // room for a second workgroup and more of the last round empty; 367 and 331 for 4096 x 4096).
@@ -849,8 +852,9 @@ static hipError_t ns_step(NsArgs& a, const NsBins& bins, hipStream_t s) {
   hipError_t e = ns_symmetric<PL, NS_GRAM>(a, bins, s);
   if (e == hipSuccess) e = ns_symmetric<PL, NS_POLY>(a, bins, s);
   if (e != hipSuccess) return e;
-  return a.last ? ns_launch<PL, NS_LAST, 2, FN, false>(a, bins, s)
-                : ns_launch<PL, NS_UPDATE, 2, FN, false>(a, bins, s);
+  if (ns_plan(a, NS_UPDATE, PL).small)
+    return a.last ? ns_launch<PL, NS_LAST, 1, 1, false>(a, bins, s) : ns_launch<PL, NS_UPDATE, 1, 1, false>(a, bins, s);
+  return a.last ? ns_launch<PL, NS_LAST, 2, FN, false>(a, bins, s) : ns_launch<PL, NS_UPDATE, 2, FN, false>(a, bins, s);
 }
 
 template <int DT, int PL>
