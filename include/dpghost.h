@@ -51,7 +51,8 @@ extern "C" {
 
 /* The version of what an existing caller relies on: it changes when an entry point, a struct
  * or a documented result does. Version 3 gained dp_clipped_grad_sum_split_workspace and
- * dp_clipped_grad_sum_grouped_ws under the same number. */
+ * dp_clipped_grad_sum_grouped_ws under the same number, and later LayerNorm, the head's losses and
+ * the orthogonalised updates. */
 #define DP_ABI_VERSION 3
 
 /* Enumerations are int-sized in both languages. Compiled as C++ they have
@@ -515,7 +516,7 @@ dp_status_t dp_clipped_grad_sum_positional_noised(const void* dE, int64_t lde, c
  * [B,T,d] (dt; row strides ldx, ldy; y may be x); gain and bias are device
  * arrays of d elements of param_dt (NULL: 1 and 0). mean and rstd (fp32
  * [B*T], either may be NULL) are what the backward pass needs.
- * Statistics are fp32. d <= 32768 (else DP_EUNSUPPORTED), B*T < 2^31. Rows of
+ * Statistics are fp32. d <= 32768 and B*T <= 2^31 - 2^16 (else DP_EUNSUPPORTED). Rows of
  * any alignment; operands may span more than 4 GiB.
  * ------------------------------------------------------------------- */
 dp_status_t dp_layernorm_forward(const void* x, int64_t ldx, const void* gain, const void* bias,
@@ -554,7 +555,7 @@ dp_status_t dp_layernorm_backward(const void* gy, int64_t ldgy, const void* x, i
  * -inf logits have probability 0; a scored row of nothing else has logp = lse
  * = -inf and a zero gradient. NaN or +inf among a row's logits makes its
  * outputs NaN, which dp_clip_factors answers with c = 0.
- * V <= 2^30 (else DP_EUNSUPPORTED), B*T < 2^31; rows of any alignment;
+ * V <= 2^30 and B*T <= 2^31 - 2^16 (else DP_EUNSUPPORTED); rows of any alignment;
  * operands may span more than 4 GiB.
  * ------------------------------------------------------------------- */
 /* logp [B,T] and (may be NULL) lse [B,T] (0 for rows that are not scored). */
@@ -595,16 +596,19 @@ dp_status_t dp_preference_loss(const void* Z, int64_t ldz, const int32_t* target
  *   X <- a_k X + b_k (X X^T) X + c_k (X X^T)^2 X      for k = 0 .. steps-1
  *   out = (accumulate ? out : 0) + scale * X_steps
  * for every matrix of the group: G [rows, cols] (in_dt, row stride ldg), out
- * [rows, cols] (out_dt, row stride ldo; may be G with its row stride and type).
- * coef is a host array of steps * 3 floats (a_k, b_k, c_k); eps >= 0 keeps a
- * zero matrix zero. With accumulate, scale = -(learning rate) updates a weight
+ * [rows, cols] (out_dt, row stride ldo; may be G with its row stride and type,
+ * but overlap no other matrix of the group).
+ * coef is a host array of steps * 3 floats (a_k, b_k, c_k); eps > 0 keeps a
+ * zero matrix zero (eps = 0 is allowed). With accumulate, scale = -(learning rate) updates a weight
  * matrix in place. NaN or inf in G makes that matrix's update NaN.
  * out_dt also chooses the products' precision: DP_F32 comes within about 1e-6
- * of exact arithmetic; DP_BF16 rounds operands to 11 bits, of the order of the result's own
- * rounding for sums under noise (1e-3 to 2e-3 of the result; more
+ * of exact arithmetic, more for long sums (3e-6 at 1601 x 6397); DP_BF16
+ * rounds the operands of matrices of more than 64 rows and columns to 11 bits, of the order of the
+ * result's own rounding for sums under noise (1e-3 to 1.5e-3 of the result; more
  * where a few directions outweigh all others: 7e-3 at 30 times their norm).
- * Singular values must stay below 8 between steps, as they do for the usual
- * coefficients (3.4445, -4.7750, 2.0315; or 15/8, -10/8, 3/8).
+ * Between steps singular values s must stay below 8 and a + b s^2 + c s^4 below
+ * 64 in magnitude, as they do for the usual coefficients (3.4445, -4.7750,
+ * 2.0315; or 15/8, -10/8, 3/8); beyond, the update becomes inf or NaN.
  * Sides up to 65536 and, padded to multiples of 128, fewer than 2^30 elements (else
  * DP_EUNSUPPORTED), 1 <= steps <= 64. The workspace is dp_orthogonalize_workspace()
  * bytes, 16-byte aligned: about 8 bytes an element of G for DP_F32 and 4 for

@@ -4,12 +4,14 @@
 
 namespace {
 
+constexpr int64_t MAX_ROWS = ((int64_t)1 << 31) - (1 << 16);  // rows are counted in 32 bits
+
 // Rows of w elements, ld apart, of a matrix of B*T rows.
 dp_status_t check_rows(int B, int T, int w, dp_dtype_t dt, const char* width) {
   if (B <= 0 || T <= 0 || w <= 0) return fail(DP_EINVAL, "B, T and %s must be positive", width);
   if (!dtype_ok(dt)) return fail(DP_EINVAL, "unknown dtype %d", (int)dt);
-  if ((int64_t)B * T > INT32_MAX)
-    return fail(DP_EUNSUPPORTED, "B*T = %lld exceeds 2^31 - 1", (long long)((int64_t)B * T));
+  if ((int64_t)B * T > MAX_ROWS)
+    return fail(DP_EUNSUPPORTED, "B*T = %lld exceeds 2^31 - 2^16", (long long)((int64_t)B * T));
   return DP_OK;
 }
 
@@ -140,7 +142,7 @@ dp_status_t dp_layernorm_forward(const void* x, int64_t ldx, const void* gain, c
 }
 
 size_t dp_layernorm_backward_workspace(int B, int T, int d) {
-  if (B <= 0 || T <= 0 || d <= 0 || d > dpg::LN_MAX_D) return 0;
+  if (B <= 0 || T <= 0 || d <= 0 || d > dpg::LN_MAX_D || (int64_t)B * T > MAX_ROWS) return 0;
   return ln_workspace(B, T, d).total;
 }
 
@@ -211,7 +213,7 @@ dp_status_t dp_cross_entropy(const void* Z, int64_t ldz, const int32_t* targets,
 }
 
 size_t dp_preference_loss_workspace(int B, int T) {
-  if (B <= 0 || T <= 0) return 0;
+  if (B <= 0 || T <= 0 || (int64_t)B * T > MAX_ROWS) return 0;
   return pref_layout(B, T).total;
 }
 
@@ -244,26 +246,16 @@ dp_status_t dp_preference_loss(const void* Z, int64_t ldz, const int32_t* target
   a.stat = reinterpret_cast<dpg::RowStat*>(ws + l.stat);
   a.w = reinterpret_cast<float*>(ws + l.slope);
   a.V = V; a.T = T; a.split = split;
-  const int64_t pairs = dpg::preference_pairs(B, T, V);
-  for (int64_t b = 0; b < B; b += pairs) {
-    const int64_t n = std::min<int64_t>(pairs, B - b);
-    a.row0 = b * T;
-    a.rows = n * T;
-    st = hip_status(dpg::launch_token_logprobs(a, kdt(dt), s), "token_logprobs launch");
-    if (st != DP_OK) return st;
-    dpg::PreferenceArgs p{};
-    p.targets = targets + a.row0; p.logp = a.logp64 + a.row0;
-    p.ref = ref_logp ? ref_logp + a.row0 : nullptr;
-    p.loss = loss + b; p.rewards = rewards ? rewards + 2 * b : nullptr;
-    p.slope = reinterpret_cast<float*>(ws + l.slope) + b;
-    p.T = T; p.V = V; p.split = split; p.beta = beta; p.smoothing = label_smoothing;
-    st = hip_status(dpg::launch_preference(p, (int)n, s), "preference launch");
-    if (st != DP_OK) return st;
-    if (!Gz) continue;
-    st = hip_status(dpg::launch_logit_grads(a, kdt(dt), s), "logit_grads launch");
-    if (st != DP_OK) return st;
-  }
-  return DP_OK;
+  a.rows = (int64_t)B * T;
+  st = hip_status(dpg::launch_token_logprobs(a, kdt(dt), s), "token_logprobs launch");
+  if (st != DP_OK) return st;
+  dpg::PreferenceArgs p{};
+  p.targets = targets; p.logp = a.logp64; p.ref = ref_logp; p.loss = loss; p.rewards = rewards;
+  p.slope = reinterpret_cast<float*>(ws + l.slope);
+  p.T = T; p.V = V; p.split = split; p.beta = beta; p.smoothing = label_smoothing;
+  st = hip_status(dpg::launch_preference(p, B, s), "preference launch");
+  if (st != DP_OK || !Gz) return st;
+  return hip_status(dpg::launch_logit_grads(a, kdt(dt), s), "logit_grads launch");
 }
 
 size_t dp_orthogonalize_workspace(const dp_matrix_t* matrices, int n, dp_dtype_t out_dt) {

@@ -422,6 +422,10 @@ struct PosSumArgs {
 };
 hipError_t launch_pos_sum(const PosSumArgs& a, int dt, hipStream_t s);
 
+// A launch counts its threads in 32 bits; the row-wise kernels below are launched for at
+// most this many workgroups of up to 1024 threads at a time.
+constexpr int64_t MAX_GROUPS = (int64_t)1 << 21;
+
 // ---------------------------------------------------------------- LayerNorm
 constexpr int LN_MAX_D = 32768;     // a row is held in the registers of at most 16 waves
 struct LnForwardArgs {
@@ -451,6 +455,7 @@ struct LnBackwardArgs {
   float* sq;            // [B, chunks] partial squares (ranges > 1)
   int64_t ldgy, ldx, lddx;
   int32_t B, T, d, param_dt;
+  int32_t b0;           // first example of the launch
   int32_t ranges, span; // an example's rows are cut into `ranges` of `span`
   int32_t chunks;       // workgroups per example of the second launch
   int32_t accumulate_dx, accumulate;
@@ -468,11 +473,11 @@ inline LnPlan ln_plan(int B, int T, int d, bool grads) {
   const int teams = d <= 2048 ? 8 : 1;
   const int least = grads ? (teams > 1 ? 2 * teams : 8) : teams;
   const int groups = d <= 2048 ? LN_GROUPS : d <= 4096 ? 4 * LN_GROUPS : LN_GROUPS;
-  int64_t ranges = (groups + B - 1) / B, most = (T + least - 1) / least;
+  int64_t ranges = ((int64_t)groups + B - 1) / B, most = ((int64_t)T + least - 1) / least;
   if (ranges > most) ranges = most;
   LnPlan p;
   p.span = (int32_t)((T + ranges - 1) / ranges);
-  p.ranges = (T + p.span - 1) / p.span;
+  p.ranges = (int32_t)(((int64_t)T + p.span - 1) / p.span);
   // One workgroup per example adds few ranges (a chain of loads each); more are added by
   // chunks of 64 features, and an example's norm by a third launch.
   p.chunks = p.ranges <= LN_FEW ? 1 : (d + 63) / 64;
@@ -509,17 +514,10 @@ struct PreferenceArgs {
   float* loss;          // [B]
   float* rewards;       // nullable [B, 2]
   float* slope;         // [B] -d loss / d log p of a chosen answer's token
-  int32_t T, V, split;
+  int32_t T, V, split, b0;  // b0: first pair of the launch
   float beta, smoothing;
 };
-// Pairs of one pass: workgroups are counted in 32 bits. (Fewer at a time, so that the second
-// read meets the memory-side cache, was no gain: 16 pairs of 1024 rows of 50257 in bf16 take 652 us in
-// one pass, 688 two at a time, 832 one by one, for the launches' ends.)
-inline int64_t preference_pairs(int B, int T, int V) {
-  const int64_t most = ((int64_t)1 << 30) / ((int64_t)T * ((V + 8191) / 8192));
-  return most < 1 ? 1 : most < B ? most : B;
-}
-hipError_t launch_preference(const PreferenceArgs& a, int B, hipStream_t s);
+hipError_t launch_preference(PreferenceArgs a, int B, hipStream_t s);
 
 // ---------------------------------------------------- orthogonalised updates
 constexpr int NS_TILE = 128;        // rows and columns of an output tile; sizes are padded to it

@@ -141,10 +141,11 @@ __global__ __launch_bounds__(LnTeam<W>::THREADS) void ln_backward_kernel(LnBackw
   __shared__ float sq_red[LnTeam<W>::THREADS / WAVE];
   const int lane = (int)threadIdx.x % LANES, team = (int)threadIdx.x / LANES;
   const uint32_t item = xcd_remap(blockIdx.x, gridDim.x);
-  const int b = (int)(item / (uint32_t)a.ranges), s = (int)(item - (uint32_t)b * a.ranges);
+  const int bl = (int)(item / (uint32_t)a.ranges), s = (int)(item - (uint32_t)bl * a.ranges);
+  const int b = a.b0 + bl;
   const int d = a.d;
   const float inv_d = 1.f / (float)d;
-  const int t0 = s * a.span, t1 = min(t0 + a.span, a.T);
+  const int t0 = s * a.span, t1 = t0 + min(a.span, a.T - t0);
   const int64_t row0 = (int64_t)b * a.T;
   Oct<DT> x[NV], g[NV];
   float mean = 0.f, rstd = 0.f;
@@ -350,16 +351,22 @@ static hipError_t ln_forward(const LnForwardArgs& a, hipStream_t s) {
 }
 
 template <int DT, int W, int NV>
-static hipError_t ln_backward(const LnBackwardArgs& a, hipStream_t s) {
-  const dim3 grid((unsigned)((int64_t)a.B * a.ranges)), block(LnTeam<W>::THREADS);
+static hipError_t ln_backward(LnBackwardArgs a, hipStream_t s) {
+  const dim3 block(LnTeam<W>::THREADS);
   const bool wg = a.dgain || a.dbias;
-  if (a.dx && wg)
-    hipLaunchKernelGGL((ln_backward_kernel<DT, W, NV, true, true>), grid, block, 0, s, a);
-  else if (a.dx)
-    hipLaunchKernelGGL((ln_backward_kernel<DT, W, NV, true, false>), grid, block, 0, s, a);
-  else
-    hipLaunchKernelGGL((ln_backward_kernel<DT, W, NV, false, true>), grid, block, 0, s, a);
-  hipError_t e = hipGetLastError();
+  hipError_t e = hipSuccess;
+  const int most = (int)(MAX_GROUPS / a.ranges);   // examples of a launch
+  for (int64_t b0 = 0; b0 < a.B && e == hipSuccess; b0 += most) {
+    a.b0 = (int)b0;
+    const dim3 grid((unsigned)((a.B - b0 < most ? a.B - b0 : most) * a.ranges));
+    if (a.dx && wg)
+      hipLaunchKernelGGL((ln_backward_kernel<DT, W, NV, true, true>), grid, block, 0, s, a);
+    else if (a.dx)
+      hipLaunchKernelGGL((ln_backward_kernel<DT, W, NV, true, false>), grid, block, 0, s, a);
+    else
+      hipLaunchKernelGGL((ln_backward_kernel<DT, W, NV, false, true>), grid, block, 0, s, a);
+    e = hipGetLastError();
+  }
   if (e != hipSuccess || a.ranges == 1 || !wg) return e;
   const dim3 fin(LN_FIN_THREADS);
   if (a.chunks == 1) {

@@ -16,7 +16,9 @@
 // keeps its row in registers between the sum and the gradient, so the logits
 // are read once (a row of 50257 is 98 KB in bf16: 8 octets a thread of
 // 1024). A pair's weight needs the last row's log p before the first row's
-// gradient, so there the logits are passed twice.
+// gradient, so there the logits are passed twice. (Fewer pairs at a time, so that the second
+// read meets the memory-side cache, was no gain: 16 pairs of 1024 rows of 50257 in bf16 took 652 us in
+// one pass, 688 two at a time, 832 one by one, for the launches' ends.)
 //
 // Sums are fp32 from the row's largest logit; the logarithm, and the sums of
 // log-ratios over an answer's tokens, are in double: a margin is a small
@@ -242,8 +244,9 @@ __global__ __launch_bounds__(LossTeam<W>::THREADS, DT == DT_BF16 ? 8 : 4) void c
   __shared__ float zt_s[LossTeam<W>::TEAMS];
   constexpr int LANES = W * WAVE, ES = Oct<DT>::ES;
   const int lane = (int)threadIdx.x % LANES, team = (int)threadIdx.x / LANES;
-  const int64_t row = (int64_t)blockIdx.x * LossTeam<W>::TEAMS + team;
-  if (row >= a.rows) return;
+  const int64_t r = (int64_t)blockIdx.x * LossTeam<W>::TEAMS + team;
+  if (r >= a.rows) return;
+  const int64_t row = a.row0 + r;
   const int V = a.V, y = a.targets[row];
   const char* z = (const char*)a.Z + row * a.ldz * ES;
   char* g = (char*)a.Gz + row * a.ldg * ES;
@@ -365,7 +368,7 @@ __global__ __launch_bounds__(LG_THREADS) void logit_grads_kernel(LossArgs a, uin
 constexpr int PF_THREADS = 256;
 __global__ __launch_bounds__(PF_THREADS) void preference_kernel(PreferenceArgs a) {
   __shared__ double red[2][PF_THREADS / WAVE];
-  const int64_t b = blockIdx.x;
+  const int64_t b = a.b0 + (int64_t)blockIdx.x;
   double c = 0.0, r = 0.0;
   for (int t = (int)threadIdx.x; t < a.T; t += PF_THREADS) {
     const int64_t row = b * a.T + t;
@@ -404,13 +407,27 @@ __global__ __launch_bounds__(PF_THREADS) void preference_kernel(PreferenceArgs a
   a.slope[b] = (float)(beta * ((1.0 - eps) * down - eps * up));
 }
 
+// Calls launch(args, groups) for slabs of rows, each of `per` to a workgroup.
+template <typename F>
+static hipError_t by_rows(LossArgs a, int64_t per, F launch) {
+  const int64_t all = a.rows, most = MAX_GROUPS * per;
+  for (int64_t done = 0; done < all; done += most) {
+    a.rows = all - done < most ? all - done : most;
+    launch(a, dim3((unsigned)((a.rows + per - 1) / per)));
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    a.row0 += a.rows;
+  }
+  return hipSuccess;
+}
+
 template <int DT, int W, int U>
 static hipError_t tl(const LossArgs& a, hipStream_t s) {
-  constexpr int TEAMS = LossTeam<W>::TEAMS;
-  const dim3 grid((unsigned)((a.rows + TEAMS - 1) / TEAMS)), block(LossTeam<W>::THREADS);
-  if (a.logp64) hipLaunchKernelGGL((token_logprobs_kernel<DT, W, U, true>), grid, block, 0, s, a);
-  else hipLaunchKernelGGL((token_logprobs_kernel<DT, W, U, false>), grid, block, 0, s, a);
-  return hipGetLastError();
+  const dim3 block(LossTeam<W>::THREADS);
+  return by_rows(a, LossTeam<W>::TEAMS, [&](const LossArgs& q, dim3 grid) {
+    if (q.logp64) hipLaunchKernelGGL((token_logprobs_kernel<DT, W, U, true>), grid, block, 0, s, q);
+    else hipLaunchKernelGGL((token_logprobs_kernel<DT, W, U, false>), grid, block, 0, s, q);
+  });
 }
 
 // Threads of a row: a wave up to 2048 logits, 4 waves up to 8192. Above, 4 where there are
@@ -429,10 +446,9 @@ hipError_t launch_token_logprobs(const LossArgs& a, int dt, hipStream_t s) {
 
 template <int DT, int W, int NV, bool NT>
 static hipError_t ce(const LossArgs& a, hipStream_t s) {
-  const unsigned teams = LossTeam<W>::TEAMS;
-  hipLaunchKernelGGL((cross_entropy_kernel<DT, W, NV, NT>),
-                     dim3((unsigned)((a.rows + teams - 1) / teams)), dim3(LossTeam<W>::THREADS), 0, s, a);
-  return hipGetLastError();
+  return by_rows(a, LossTeam<W>::TEAMS, [&](const LossArgs& q, dim3 grid) {
+    hipLaunchKernelGGL((cross_entropy_kernel<DT, W, NV, NT>), grid, dim3(LossTeam<W>::THREADS), 0, s, q);
+  });
 }
 
 template <int DT, bool NT>
@@ -458,11 +474,18 @@ hipError_t launch_cross_entropy(const LossArgs& a, int dt, hipStream_t s) {
 }
 
 template <int DT, bool NT>
-static hipError_t lg(const LossArgs& a, hipStream_t s) {
+static hipError_t lg(LossArgs a, hipStream_t s) {
   const uint32_t parts = (uint32_t)((((int64_t)a.V + 7) / 8 + LG_OCTETS - 1) / LG_OCTETS);
-  const dim3 grid((unsigned)(a.rows * parts)), block(LG_THREADS);
-  hipLaunchKernelGGL((logit_grads_kernel<DT, NT>), grid, block, 0, s, a, parts);
-  return hipGetLastError();
+  const int64_t all = a.rows, most = 4 * MAX_GROUPS / parts;   // V <= 2^30: at least 64
+  for (int64_t done = 0; done < all; done += most) {
+    a.rows = all - done < most ? all - done : most;
+    const dim3 grid((unsigned)(a.rows * parts));
+    hipLaunchKernelGGL((logit_grads_kernel<DT, NT>), grid, dim3(LG_THREADS), 0, s, a, parts);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    a.row0 += a.rows;
+  }
+  return hipSuccess;
 }
 
 hipError_t launch_logit_grads(const LossArgs& a, int dt, hipStream_t s) {
@@ -471,9 +494,15 @@ hipError_t launch_logit_grads(const LossArgs& a, int dt, hipStream_t s) {
   return lg<DT_F32, false>(a, s);
 }
 
-hipError_t launch_preference(const PreferenceArgs& a, int B, hipStream_t s) {
-  hipLaunchKernelGGL(preference_kernel, dim3((unsigned)B), dim3(PF_THREADS), 0, s, a);
-  return hipGetLastError();
+hipError_t launch_preference(PreferenceArgs a, int B, hipStream_t s) {
+  for (int64_t b0 = 0; b0 < B; b0 += MAX_GROUPS) {
+    a.b0 = (int32_t)b0;
+    const int64_t n = B - b0 < MAX_GROUPS ? B - b0 : MAX_GROUPS;
+    hipLaunchKernelGGL(preference_kernel, dim3((unsigned)n), dim3(PF_THREADS), 0, s, a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 }  // namespace dpg

@@ -348,3 +348,31 @@ def test_on_another_stream(dp):
     dp.dp_layernorm_backward(gy, x, None, mean, rstd, None, dgain=g[1])
     torch.cuda.synchronize()
     assert torch.equal(g[0], g[1])
+
+
+def test_more_rows_than_one_launch_takes(dp):
+    """70 million rows of two logits, and 8.5 million examples of one token."""
+    n = 70_000_000
+    z = torch.zeros(1, n, 2, dtype=torch.bfloat16, device="cuda")
+    at = [0, 8_388_607, 8_388_608, n // 2, n - 1]
+    for k, r in enumerate(at):
+        z[0, r, 1] = 1.0 + k
+    y = torch.ones(1, n, dtype=torch.int32, device="cuda")
+    w = torch.ones(1, n, device="cuda")
+    logp, lse = torch.full((1, n), 9.0, device="cuda"), torch.full((1, n), 9.0, device="cuda")
+    dp.dp_token_logprobs(z, y, logp, lse=lse)
+    want = -np.log1p(np.exp(-(1.0 + np.arange(len(at)))))
+    assert np.abs(_host(logp[0, at]) - want).max() < 1e-6
+    assert abs(float(logp.double().sum()) - (want.sum() - (n - len(at)) * np.log(2.0))) < 1e-6 * n
+    dp.dp_cross_entropy(z, y, w, logp, z)
+    assert np.abs(_host(z[0, at, 1]) - (np.exp(want) - 1)).max() <= 2.0 ** -8
+    assert int((z[0, :, 1] == -0.5).sum()) == n - len(at) and int((z[0, :, 0] == 0.5).sum()) == n - len(at)
+    del z, y, w, logp, lse
+    B, d = 8_500_000, 8
+    x = torch.arange(d, device="cuda").float().expand(B, 1, d).contiguous()
+    gy = torch.zeros(B, 1, d, device="cuda")
+    gy[:, 0, 3] = torch.arange(B, device="cuda") % 7 + 1.0
+    mean, rstd = torch.full((B, 1), 3.5, device="cuda"), torch.full((B, 1), 0.5, device="cuda")
+    dbias, n2 = torch.full((B, d), 9.0, device="cuda"), torch.full((B,), 9.0, device="cuda")
+    dp.dp_layernorm_backward(gy, x, None, mean, rstd, None, dbias=dbias, norm2=n2)
+    assert torch.equal(dbias, gy[:, 0]) and torch.equal(n2, gy[:, 0, 3] ** 2)

@@ -35,6 +35,7 @@ def _forward(L, **kw):
     (dict(d=0), EINVAL), (dict(dt=2), EINVAL), (dict(pdt=7), EINVAL), (dict(ldx=63), EINVAL),
     (dict(ldy=63), EINVAL), (dict(eps=-1.0), EINVAL), (dict(eps=float("nan")), EINVAL),
     (dict(y=P[0], ldy=128), EINVAL), (dict(B=1 << 16, T=1 << 16), EUNSUP),
+    (dict(B=1, T=2 ** 31 - 2 ** 16 + 1), EUNSUP),
     (dict(d=32769, ldx=32769, ldy=32769), EUNSUP)])
 def test_layernorm_forward_refuses(L, kw, status):
     assert _forward(L, **kw) == status, L.dp_last_error()
@@ -66,6 +67,10 @@ def test_layernorm_workspace(L):
     assert f(0, 16, 64) == f(4, 0, 64) == f(4, 16, 0) == f(4, 16, 40000) == 0
     assert f(1, 4096, 768) >= 2 * 768 * 4          # ranges of a long example
     assert f(2000, 128, 768) == 0                  # enough examples to fill the GPU
+    most = 2 ** 31 - 2 ** 16                       # the longest: sizes do not overflow
+    assert f(most, 1, 8) == 0 and 0 < f(1, most, 8) < 1 << 20
+    assert f(1, most + 1, 8) == f(most + 1, 1, 8) == 0
+    assert L.dp_preference_loss_workspace(1, most) >= 16 * most
 
 
 def _losses(L, which, **kw):
