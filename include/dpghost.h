@@ -602,7 +602,7 @@ dp_status_t dp_preference_loss(const void* Z, int64_t ldz, const int32_t* target
  * zero matrix zero (eps = 0 is allowed). With accumulate, scale = -(learning rate) updates a weight
  * matrix in place. NaN or inf in G makes that matrix's update NaN.
  * out_dt also chooses the products' precision: DP_F32 comes within about 1e-6
- * of exact arithmetic, more for long sums (3e-6 at 1601 x 6397); DP_BF16
+ * (as a norm) of exact arithmetic, 2e-6 for small matrices; DP_BF16
  * rounds the operands of matrices of more than 64 rows and columns to 11 bits, of the order of the
  * result's own rounding for sums under noise (1e-3 to 1.5e-3 of the result; more
  * where a few directions outweigh all others: 7e-3 at 30 times their norm).

@@ -17,7 +17,7 @@
 //     size of what lies beside G's leading directions: 3e-3 at 10, 7e-3 at 30.)
 //   PL = 2 (fp32 results): two planes, x = x0 + x1 with x1 what is left (22 bits
 //     together), and the three products x0 y0 + x0 y1 + x1 y0; x1 y1 is below
-//     2^-22. About 3e-7 in all.
+//     2^-22. 0.6e-6 to 1.9e-6 in all (32-bit library products: 1.3e-6 to 4.4e-6).
 // Sums are fp32 in the matrix cores, the Frobenius norm is in fp64.
 //
 // Layout: m and n are padded with zeros to multiples of a tile, so that the
@@ -421,11 +421,17 @@ __global__ __launch_bounds__(256, (NsShape<PL, FM, FN>::GROUPS)) void ns_gemm_ke
     for (int h = 0; h < 2; ++h) fo[h] = (uint32_t)(fr * ROWB + (((2 * h + (lane >> 5)) ^ fx) << 4));
   }
 
-  f32x16 acc[FM][FN];
+  // With two planes the small products have a sum of their own: the matrix core cuts what
+  // lies below a fixed distance from a sum's largest term, towards zero, so that every product on
+  // the running sum costs a long one some of its last bits.
+  f32x16 acc[FM][FN], little[PL == 2 ? FM : 1][PL == 2 ? FN : 1];
 #pragma unroll
   for (int i = 0; i < FM; ++i)
 #pragma unroll
-    for (int j = 0; j < FN; ++j) acc[i][j] = f32x16{};
+    for (int j = 0; j < FN; ++j) {
+      acc[i][j] = f32x16{};
+      if constexpr (PL == 2) little[i][j] = f32x16{};
+    }
 
   struct Frags {
     u32x4 p[PL][FM], q[PL][FN];
@@ -459,7 +465,8 @@ __global__ __launch_bounds__(256, (NsShape<PL, FM, FN>::GROUPS)) void ns_gemm_ke
       const int t = k / (FM * FN), i = (k / FN) % FM, j = k % FN;
       // small products first: x1 y0, x0 y1, then x0 y0
       const int pq = TERMS == 3 && t == 0 ? 1 : 0, pp = TERMS == 3 && t == 1 ? 1 : 0;
-      acc[i][j] = mfma32_f16(f.p[pp][i], f.q[pq][j], acc[i][j]);
+      f32x16& to = t < TERMS - 1 ? little[PL == 2 ? i : 0][PL == 2 ? j : 0] : acc[i][j];
+      to = mfma32_f16(f.p[pp][i], f.q[pq][j], to);
 #pragma unroll
       for (int r = 0; r < READS; ++r)
         if (r * MF / READS == k) read(nx, st, h, r);
@@ -493,6 +500,12 @@ __global__ __launch_bounds__(256, (NsShape<PL, FM, FN>::GROUPS)) void ns_gemm_ke
     __builtin_amdgcn_sched_barrier(0);
     half(f1, f0, ring + next * STAGE, 0, s + RING - 1, true);
     slot = next;
+  }
+  if constexpr (PL == 2) {
+#pragma unroll
+    for (int i = 0; i < FM; ++i)
+#pragma unroll
+      for (int j = 0; j < FN; ++j) acc[i][j] += little[i][j];
   }
   if constexpr (PART) {   // the raw sums, four floats of every lane at a time
 #pragma unroll
