@@ -587,32 +587,50 @@ DPG_HD inline size_t ns_bytes(int mp, int np, int pl) {
 // sooner: 6 us and US_K_SMALL per k, 512 at a time with one plane and 256 with two (their rings). All five
 // steps, us, large and small: 600 x 600 fp32 results 251, 153; bf16 188, 116; 1536 x 1536 bf16 350, 269;
 // and 100 x 3000 fp32, X X^T alone small: 144, 210; 1536 x 1536 fp32, updates alone: 419, 451.
+// Updates and X X^T with one plane that fill a round with 256 x 256 tiles take those: fewer LDS reads and
+// loads per product (us, such tiles and the others: updates 4096 x 4096 120, 131; 24 x (1024 x 1024, 1024 x
+// 4096) 281, 312; their X X^T 167, 184). A^2, whose other operand needs registers too, does not: 115, 95.
 struct NsPlan {
   int ks;
-  bool small;
+  bool small, wide;       // 64 x 64 tiles; 256 x 256 tiles
 };
 constexpr double NS_JOIN_US = 8.0;
 inline NsPlan ns_plan(const NsArgs& a, int kind, int pl) {
   const bool sym = kind == NS_GRAM || kind == NS_POLY;
-  const double us_k = pl == 2 ? 0.0136 : sym ? 0.008 : 0.010, us_k_small = pl == 2 ? 0.0067 : 0.0045;
+  const double us_k = pl == 2 ? 0.0136 : sym ? 0.008 : 0.0139, us_k_small = pl == 2 ? 0.0067 : 0.0045;
+  const double us_k_wide = 0.0256;
   const int64_t at_once = pl == 2 ? 256 : 512;
-  int64_t tiles = 0, few = 0, k_most = 0, k_least = 1 << 30;   // few: large tiles
+  int64_t tiles = 0, few = 0, wide = 0, k_most = 0, k_least = 1 << 30;   // few: large tiles
+  double few_k = 0.0, wide_k = 0.0;                                     // and the sum of their costs in k
   for (int l = 0; l < a.n; ++l) {
     const int64_t m = a.M[l].mp / 64, n = a.M[l].np / 64, k = kind == NS_GRAM ? a.M[l].np : a.M[l].mp;
+    const int64_t mw = (m + 3) / 4, nw = (n + 3) / 4;
+    const int64_t f = sym ? m / 2 * (m / 2 + 1) / 2 : m / 2 * ((n / 2 + 2 - pl) / (3 - pl));
+    const int64_t w = sym ? mw * (mw + 1) / 2 : mw * nw;
     tiles += sym ? m * (m + 1) / 2 : m * n;
-    few += sym ? m / 2 * (m / 2 + 1) / 2 : m / 2 * ((n / 2 + 2 - pl) / (3 - pl));
+    few += f;
+    wide += w;
+    few_k += (double)f * (double)(k + 600);
+    wide_k += (double)w * (double)(k + 600);
     k_most = k > k_most ? k : k_most;
     k_least = k < k_least ? k : k_least;
   }
-  NsPlan best{1, false};
-  double best_us = (double)((few + 255) / 256) * (double)(k_most + 600) * us_k;
+  // Items of one length end in whole rounds; longer ones first, shorter ones fill the last.
+  auto rounds_k = [&](int64_t items, double sum) {
+    if (k_most == k_least) return (double)((items + 255) / 256) * (double)(k_most + 600);
+    return sum / 256 > (double)(k_most + 600) ? sum / 256 : (double)(k_most + 600);
+  };
+  NsPlan best{1, false, false};
+  double best_us = rounds_k(few, few_k) * us_k;
   if (sym && few <= 128)
     for (int ks = 2; ks <= 16 && ks * 128 <= k_least; ++ks) {
       const double us = (double)((few * ks + 255) / 256) * ((double)k_most / ks + 600) * us_k + NS_JOIN_US;
       if (us < 0.95 * best_us) { best_us = us; best.ks = ks; }
     }
   const int64_t rounds = (tiles + at_once - 1) / at_once;
-  if (rounds <= 2 && 6.0 + (double)rounds * (double)k_most * us_k_small < 1.1 * best_us) best = NsPlan{1, true};
+  if (rounds <= 2 && 6.0 + (double)rounds * (double)k_most * us_k_small < 1.1 * best_us) return NsPlan{1, true, false};
+  if (pl == 1 && (kind == NS_GRAM || kind == NS_UPDATE) && wide >= 256 && rounds_k(wide, wide_k) * us_k_wide < 1.02 * best_us)
+    return NsPlan{1, false, true};
   return best;
 }
 inline size_t ns_part_bytes(const NsArgs& a, int pl) {

@@ -843,6 +843,8 @@ static hipError_t ns_symmetric(NsArgs& a, const NsBins& bins, hipStream_t s) {
   const NsPlan plan = ns_plan(a, KIND, PL);
   a.ks = plan.ks;
   if (plan.small) return ns_launch<PL, KIND, 1, 1, false>(a, bins, s);
+  if constexpr (PL == 1 && KIND == NS_GRAM)
+    if (plan.wide) return ns_launch<PL, KIND, 4, 4, false>(a, bins, s);
   if (a.ks == 1) return ns_launch<PL, KIND, 2, 2, false>(a, bins, s);
   const hipError_t e = ns_launch<PL, KIND, 2, 2, true>(a, bins, s);
   if (e != hipSuccess) return e;
@@ -857,17 +859,22 @@ static hipError_t ns_symmetric(NsArgs& a, const NsBins& bins, hipStream_t s) {
 
 // Large tiles: 128 x 128 for the symmetric products, whose launches have few; for updates
 // 128 x 256 with one plane (fewer LDS reads per product: 171 us for GPT-2's blocks, 197 with 128 x
-// 128), 128 x 128 with two (105 us for 1601 x 6397, 116 with 256 x 128, which leave no
-// room for a second workgroup and more of the last round empty; 367 and 331 for 4096 x 4096).
+// 128), the last 190 us (200 with 256 x 256, which waits for its stores), 128 x 128 with two (105 us
+// for 1601 x 6397, 116 with 256 x 128, which leave no room for a second workgroup and more of the last
+// round empty; 367 and 331 for 4096 x 4096).
 template <int PL>
 static hipError_t ns_step(NsArgs& a, const NsBins& bins, hipStream_t s) {
   constexpr int FN = PL == 1 ? 4 : 2;
   hipError_t e = ns_symmetric<PL, NS_GRAM>(a, bins, s);
   if (e == hipSuccess) e = ns_symmetric<PL, NS_POLY>(a, bins, s);
   if (e != hipSuccess) return e;
-  if (ns_plan(a, NS_UPDATE, PL).small)
-    return a.last ? ns_launch<PL, NS_LAST, 1, 1, false>(a, bins, s) : ns_launch<PL, NS_UPDATE, 1, 1, false>(a, bins, s);
-  return a.last ? ns_launch<PL, NS_LAST, 2, FN, false>(a, bins, s) : ns_launch<PL, NS_UPDATE, 2, FN, false>(a, bins, s);
+  const NsPlan plan = ns_plan(a, a.last ? NS_LAST : NS_UPDATE, PL);
+  if (a.last)
+    return plan.small ? ns_launch<PL, NS_LAST, 1, 1, false>(a, bins, s) : ns_launch<PL, NS_LAST, 2, FN, false>(a, bins, s);
+  if (plan.small) return ns_launch<PL, NS_UPDATE, 1, 1, false>(a, bins, s);
+  if constexpr (PL == 1)
+    if (plan.wide) return ns_launch<PL, NS_UPDATE, 4, 4, false>(a, bins, s);
+  return ns_launch<PL, NS_UPDATE, 2, FN, false>(a, bins, s);
 }
 
 template <int DT, int PL>

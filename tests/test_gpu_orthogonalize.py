@@ -100,6 +100,19 @@ def test_step_counts_and_coefficients_per_step(dp):
     assert float((x @ x.T - torch.eye(90, device="cuda", dtype=torch.float64)).abs().max()) < 90 * 2.0 ** -20
 
 
+@pytest.mark.parametrize("n,r,c", [(48, 1200, 650), (14, 1850, 1950)])
+def test_many_larger_matrices(dp, n, r, c):
+    """Enough output for the largest tiles, whose last rows and columns reach past the matrix."""
+    grads = [_matrix(k, r, c, "bf16") for k in range(n)]
+    outs = [torch.empty_like(g) for g in grads]
+    dp.dp_orthogonalize_grouped(grads, outs)
+    for k in (0, n - 1):
+        _check(outs[k], grads[k], [MUON] * 5, 1e-7, "bf16", f"matrix {k} of {n}")
+    for k in range(1, n - 1):      # the rest: rows (or columns) of like length, as the two checked
+        x = outs[k].float()
+        assert torch.isfinite(x).all() and abs(float(x.norm() / outs[0].float().norm()) - 1) < 0.05, k
+
+
 @pytest.mark.parametrize("out", ["f32", "bf16"])
 def test_scaled_onto_a_prior_and_in_place(dp, out):
     shapes = [(130, 70), (70, 130)]
