@@ -14,7 +14,7 @@
 // All of it is bound by HBM: a logit costs one exponential (three in the
 // passes that write gradients twice over) and moves 2 to 8 bytes. Cross-entropy
 // keeps its row in registers between the sum and the gradient, so the logits
-// are read once (a row of 50257 is 98 KB in bf16: 8 octets a thread of
+// are read once (a row of 50257 is 98 KB in bf16: 7 units of 16 bytes a thread of
 // 1024). A pair's weight needs the last row's log p before the first row's
 // gradient, so there the logits are passed twice. (Fewer pairs at a time, so that the second
 // read meets the memory-side cache, was no gain: 16 pairs of 1024 rows of 50257 in bf16 took 652 us in
@@ -130,32 +130,41 @@ struct RunningSum<true> {
   }
 };
 
-// That of the lane's logits: octets `lane`, `lane` + LANES, ... of the row, U of them in
-// flight. EXACT rows are read a second time soon, others take streaming loads in bf16 (24 x 128
-// rows of 50257: 57 us without the hint, 55 with; in fp32, where a lane's octet is two loads of the
-// same line, 83 and 101).
+// Elements by which a row starts behind a 16-byte boundary. Its units are counted from there,
+// unit u the N elements from N u - phase on, so that every whole one is an aligned access
+// wherever the row starts and neighbouring lanes never share a line (rows of 50257 in bf16,
+// one behind the other, so counted and from the row's start: 24 x 128 log-probabilities 47 and 55 us, their
+// cross-entropy 106 and 138, a preference loss of 8 x 512 tokens 172 and 212).
+template <int DT>
+__device__ __forceinline__ int row_phase(const char* z) {
+  return (int)((uintptr_t)z & 15) / Unit<DT>::ES;
+}
+
+// That of the lane's logits: units `lane`, `lane` + LANES, ... of the row, U of them in
+// flight. EXACT rows are read a second time soon, others take streaming loads.
 template <int DT, int W, int U, bool EXACT>
 __device__ __forceinline__ RunningSum<EXACT> row_sum(const char* z, int V, int lane) {
-  constexpr int LANES = W * WAVE;
+  constexpr int LANES = W * WAVE, N = Unit<DT>::N;
+  const int phase = row_phase<DT>(z);
   RunningSum<EXACT> s;
-  for (int o = lane; o * 8 < V; o += U * LANES) {
-    Oct<DT> v[U];
+  for (int o = lane; o * N - phase < V; o += U * LANES) {
+    Unit<DT> v[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int col = (o + u * LANES) * 8;
-      v[u].template load<!EXACT && DT == DT_BF16>(z + (int64_t)col * Oct<DT>::ES, V - col, NEG_INF<DT>);
+      const int col = (o + u * LANES) * N - phase;
+      v[u].template load<!EXACT>(z + (int64_t)col * Unit<DT>::ES, V - col, NEG_INF<DT>, u ? 0 : -col);
     }
     float m = s.top;
 #pragma unroll
     for (int u = 0; u < U; ++u)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) m = fmaxf(m, v[u].at(e));
+      for (int e = 0; e < N; ++e) m = fmaxf(m, v[u].at(e));
     s.move(m);
     float part = 0.f, slope = 0.f;
 #pragma unroll
     for (int u = 0; u < U; ++u)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
+      for (int e = 0; e < N; ++e) {
         const float d = v[u].at(e) - m, x = exp_of(d);
         part += x;
         if constexpr (EXACT) slope = fmaf(fmaxf(d, -200.f), x, slope);   // x is 0 below
@@ -192,7 +201,7 @@ __global__ __launch_bounds__(LossTeam<W>::THREADS) void token_logprobs_kernel(Lo
     }
     return;
   }
-  const char* z = (const char*)a.Z + row * a.ldz * Oct<DT>::ES;
+  const char* z = (const char*)a.Z + row * a.ldz * Unit<DT>::ES;
   const float zt = logit_at<DT>(z, y);
   RunningSum<EXACT> s = row_sum<DT, W, U, EXACT>(z, a.V, lane);
   s.template meet<W>(red);
@@ -205,13 +214,13 @@ __global__ __launch_bounds__(LossTeam<W>::THREADS) void token_logprobs_kernel(Lo
   }
 }
 
-// Eight gradients w p of an octet, f = w / sum. The target's is put right afterwards, by
+// The gradients w p of a unit, f = w / sum. The target's is put right afterwards, by
 // the thread that stored it.
 template <int DT>
-__device__ __forceinline__ void grad_octet(Oct<DT>& v, float top, float f) {
-  float o[8];
+__device__ __forceinline__ void grad_unit(Unit<DT>& v, float top, float f) {
+  float o[Unit<DT>::N];
 #pragma unroll
-  for (int e = 0; e < 8; ++e) o[e] = exp_of(v.at(e) - top) * f;
+  for (int e = 0; e < Unit<DT>::N; ++e) o[e] = exp_of(v.at(e) - top) * f;
   v.set(o);
 }
 template <int DT>
@@ -223,26 +232,26 @@ __device__ __forceinline__ void grad_target(char* g, int y, float zt, float top,
     ((float*)g)[y] = v;
 }
 
-// Rows that give no gradient: octets from `lane` on, LANES apart.
+// Rows that give no gradient: units from `lane` on, LANES apart.
 template <int DT, bool NT>
 __device__ __forceinline__ void zero_row(char* g, int V, int lane, int lanes) {
-  Oct<DT> v;
-  const float none[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+  Unit<DT> v;
+  const float none[Unit<DT>::N] = {};
   v.set(none);
-  for (int col = lane * 8; col < V; col += lanes * 8) v.template store<NT>(g + (int64_t)col * Oct<DT>::ES, V - col);
+  for (int col = lane * Unit<DT>::N - row_phase<DT>(g); col < V; col += lanes * Unit<DT>::N)
+    v.template store<NT>(g + (int64_t)col * Unit<DT>::ES, V - col, -col);
 }
 
-// NV > 0: the row stays in registers, NV octets a lane. NV = 0: rows longer than
-// that are read again for the gradient. NT: streaming loads and stores, for bf16 rows of whole 16-byte
-// units (32 x 128 bf16 rows of 50257: 140 us without the hints, 129 with; 24 x 100 unaligned fp32 rows, whose
-// lines neighbouring lanes share: 165 and 197).
+// NV > 0: the row stays in registers, NV units a lane. NV = 0: rows longer than
+// that are read again for the gradient. Loads are streaming ones, and stores where their
+// units are aligned too (NT) (32 x 128 bf16 rows of 50257: 140 us without the hints, 129 with).
 // (Eight waves a SIMD: a CU then works on two rows of 16 waves, one loading while the other
 // computes.)
 template <int DT, int W, int NV, bool NT>
 __global__ __launch_bounds__(LossTeam<W>::THREADS, DT == DT_BF16 ? 8 : 4) void cross_entropy_kernel(LossArgs a) {
   __shared__ double red[2 * W];
   __shared__ float zt_s[LossTeam<W>::TEAMS];
-  constexpr int LANES = W * WAVE, ES = Oct<DT>::ES;
+  constexpr int LANES = W * WAVE, ES = Unit<DT>::ES, N = Unit<DT>::N;
   const int lane = (int)threadIdx.x % LANES, team = (int)threadIdx.x / LANES;
   const int64_t r = (int64_t)blockIdx.x * LossTeam<W>::TEAMS + team;
   if (r >= a.rows) return;
@@ -250,6 +259,7 @@ __global__ __launch_bounds__(LossTeam<W>::THREADS, DT == DT_BF16 ? 8 : 4) void c
   const int V = a.V, y = a.targets[row];
   const char* z = (const char*)a.Z + row * a.ldz * ES;
   char* g = (char*)a.Gz + row * a.ldg * ES;
+  const int phase = row_phase<DT>(z);
   if (y < 0 || y >= V) {
     if (lane == 0 && a.logp) a.logp[row] = 0.f;
     zero_row<DT, NT>(g, V, lane, LANES);
@@ -261,33 +271,31 @@ __global__ __launch_bounds__(LossTeam<W>::THREADS, DT == DT_BF16 ? 8 : 4) void c
   if (lane == 0) zt_s[team] = logit_at<DT>(z, y);
   if constexpr (W == 1) __builtin_amdgcn_wave_barrier();
   float top, sum = 0.f;
-  Oct<DT> v[NV > 0 ? NV : 1];
+  Unit<DT> v[NV > 0 ? NV : 1];
   // Makes the row opaque: unpacked values and exponentials that a later pass over it could
   // use again would be kept, in several times its registers.
   auto hide = [&]() __attribute__((always_inline)) {
 #pragma unroll
-    for (int j = 0; j < NV; ++j)
-#pragma unroll
-      for (int q = 0; q < (DT == DT_BF16 ? 1 : 2); ++q) asm volatile("" : "+v"(v[j].r[q]));
+    for (int j = 0; j < NV; ++j) asm volatile("" : "+v"(v[j].r[0]));
   };
   if constexpr (NV > 0) {
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
-      const int col = (lane + j * LANES) * 8;
-      v[j].template load<NT>(z + (int64_t)col * ES, V - col, NEG_INF<DT>);
+      const int col = (lane + j * LANES) * N - phase;
+      v[j].template load<true>(z + (int64_t)col * ES, V - col, NEG_INF<DT>, j ? 0 : -col);
     }
     top = LOWEST;
 #pragma unroll
     for (int j = 0; j < NV; ++j)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) top = fmaxf(top, v[j].at(e));
+      for (int e = 0; e < N; ++e) top = fmaxf(top, v[j].at(e));
     top = team_max<W>(top, (float*)red);
     hide();
     float none = 0.f;
 #pragma unroll
     for (int j = 0; j < NV; ++j)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) sum += exp_of(v[j].at(e) - top);
+      for (int e = 0; e < N; ++e) sum += exp_of(v[j].at(e) - top);
     team_sum2<W>(sum, none, (float*)red);
   } else {
     RunningSum<false> all = row_sum<DT, W, 4, false>(z, V, lane);
@@ -303,63 +311,67 @@ __global__ __launch_bounds__(LossTeam<W>::THREADS, DT == DT_BF16 ? 8 : 4) void c
   const float f = w / sum;
   hide();
   if constexpr (NV > 0) {
+    int first = lane * N - phase;
+    asm volatile("" : "+v"(first));   // opaque too: the units' places are found again
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
-      const int col = (lane + j * LANES) * 8;
-      grad_octet<DT>(v[j], top, f);
-      v[j].template store<NT>(g + (int64_t)col * ES, V - col);
+      const int col = first + j * LANES * N;
+      grad_unit<DT>(v[j], top, f);
+      v[j].template store<NT>(g + (int64_t)col * ES, V - col, j ? 0 : -col);
     }
   } else {
-    for (int col = lane * 8; col < V; col += LANES * 8) {
-      Oct<DT> u;
-      u.template load<NT>(z + (int64_t)col * ES, V - col, NEG_INF<DT>);
-      grad_octet<DT>(u, top, f);
-      u.template store<NT>(g + (int64_t)col * ES, V - col);
+    for (int col = lane * N - phase; col < V; col += LANES * N) {
+      Unit<DT> u;
+      u.template load<true>(z + (int64_t)col * ES, V - col, NEG_INF<DT>, -col);
+      grad_unit<DT>(u, top, f);
+      u.template store<NT>(g + (int64_t)col * ES, V - col, -col);
     }
   }
-  if ((y >> 3) % LANES == lane) grad_target<DT>(g, y, zt_s[team], top, f, w);
+  if (((y + phase) / N) % LANES == lane) grad_target<DT>(g, y, zt_s[team], top, f, w);
 }
 
 // The preference loss's gradient from the rows' statistics and the pairs'
-// slopes: workgroup = (row, LG_OCTETS octets).
-constexpr int LG_U = 4, LG_THREADS = 256, LG_OCTETS = LG_U * LG_THREADS;
+// slopes: workgroup = (row, LG_UNITS units).
+constexpr int LG_U = 4, LG_THREADS = 256, LG_UNITS = LG_U * LG_THREADS;
 template <int DT, bool NT>
 __global__ __launch_bounds__(LG_THREADS) void logit_grads_kernel(LossArgs a, uint32_t parts) {
-  constexpr int ES = Oct<DT>::ES;
+  constexpr int ES = Unit<DT>::ES, N = Unit<DT>::N;
   const uint32_t r = blockIdx.x / parts;
   const int64_t row = a.row0 + r;
   const int V = a.V, y = a.targets[row], t = (int)(row % a.T);
-  const int o0 = (int)(blockIdx.x - r * parts) * LG_OCTETS + (int)threadIdx.x;
+  const int o0 = (int)(blockIdx.x - r * parts) * LG_UNITS + (int)threadIdx.x;
   const char* z = (const char*)a.Z + row * a.ldz * ES;
   char* g = (char*)a.Gz + row * a.ldg * ES;
+  const int phase = row_phase<DT>(z);
   const RowStat st = a.stat[row];
   float w = a.w[row / a.T];
   if (t >= a.split) w = -w;
-  Oct<DT> v[LG_U];
+  Unit<DT> v[LG_U];
   if (y < 0 || y >= V || w == 0.f || st.scale == 0.f) {
-    const float none[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    const float none[N] = {};
     v[0].set(none);
 #pragma unroll
     for (int u = 0; u < LG_U; ++u) {
-      const int col = (o0 + u * LG_THREADS) * 8;
-      v[0].template store<NT>(g + (int64_t)col * ES, V - col);
+      const int col = (o0 + u * LG_THREADS) * N - phase;
+      v[0].template store<NT>(g + (int64_t)col * ES, V - col, u ? 0 : -col);
     }
     return;
   }
   const float f = w * st.scale;
   // The target's logit, by the thread that replaces it.
-  const bool mine = (y >> 3) / LG_OCTETS == (int)(blockIdx.x - r * parts) && (y >> 3) % LG_THREADS == (int)threadIdx.x;
+  const int yo = (y + phase) / N;
+  const bool mine = yo / LG_UNITS == (int)(blockIdx.x - r * parts) && yo % LG_THREADS == (int)threadIdx.x;
   const float zt = mine ? logit_at<DT>(z, y) : 0.f;
 #pragma unroll
   for (int u = 0; u < LG_U; ++u) {
-    const int col = (o0 + u * LG_THREADS) * 8;
-    v[u].template load<NT>(z + (int64_t)col * ES, V - col, NEG_INF<DT>);
+    const int col = (o0 + u * LG_THREADS) * N - phase;
+    v[u].template load<true>(z + (int64_t)col * ES, V - col, NEG_INF<DT>, u ? 0 : -col);
   }
 #pragma unroll
   for (int u = 0; u < LG_U; ++u) {
-    const int col = (o0 + u * LG_THREADS) * 8;
-    grad_octet<DT>(v[u], st.top, f);
-    v[u].template store<NT>(g + (int64_t)col * ES, V - col);
+    const int col = (o0 + u * LG_THREADS) * N - phase;
+    grad_unit<DT>(v[u], st.top, f);
+    v[u].template store<NT>(g + (int64_t)col * ES, V - col, u ? 0 : -col);
   }
   if (mine) grad_target<DT>(g, y, zt, st.top, f, w);
 }
@@ -451,31 +463,43 @@ static hipError_t ce(const LossArgs& a, hipStream_t s) {
   });
 }
 
+// Units of a row, whatever its phase (see row_phase).
+template <int DT>
+static int64_t row_units(const LossArgs& a) {
+  constexpr int N = Unit<DT>::N;
+  const bool aligned = ((uintptr_t)a.Z & 15) == 0 && (a.ldz * Unit<DT>::ES) % 16 == 0;
+  return ((int64_t)a.V + (aligned ? 0 : N - 1) + N - 1) / N;
+}
+// Whether every row's gradient has its logits' phase, so that its stores are aligned too.
+template <int DT>
+static bool same_phase(const LossArgs& a) {
+  return (((uintptr_t)a.Gz - (uintptr_t)a.Z) & 15) == 0 && ((a.ldg - a.ldz) * Unit<DT>::ES) % 16 == 0;
+}
+
 template <int DT, bool NT>
 static hipError_t ce_by_width(const LossArgs& a, hipStream_t s) {
-  const int octs = (a.V + 7) / 8;
-  if (octs <= 64) return ce<DT, 1, 1, NT>(a, s);
-  if (octs <= 256) return ce<DT, 1, 4, NT>(a, s);
-  if (octs <= 1024) return ce<DT, 4, 4, NT>(a, s);
-  if (octs <= 4096) return ce<DT, 16, 4, NT>(a, s);
-  if (octs <= 7168) return ce<DT, 16, 7, NT>(a, s);
+  const int64_t units = row_units<DT>(a);
+  constexpr int F = 8 / Unit<DT>::N;   // units per 8 elements
+  if (units <= 64 * F) return ce<DT, 1, F, NT>(a, s);
+  if (units <= 256 * F) return ce<DT, 1, 4 * F, NT>(a, s);
+  if (units <= 1024 * F) return ce<DT, 4, 4 * F, NT>(a, s);
+  if (units <= 4096 * F) return ce<DT, 16, 4 * F, NT>(a, s);
+  if (units <= 7168 * F) return ce<DT, 16, 7 * F, NT>(a, s);
   return ce<DT, 16, 0, NT>(a, s);
 }
 
-// Whether every row of the logits and of the gradient starts on a 16-byte boundary.
-static bool aligned_rows(const LossArgs& a, int es) {
-  return (((uintptr_t)a.Gz | (uintptr_t)a.Z) & 15) == 0 && (a.ldg * es) % 16 == 0 && (a.ldz * es) % 16 == 0;
+template <int DT>
+static hipError_t ce_by_type(const LossArgs& a, hipStream_t s) {
+  return same_phase<DT>(a) ? ce_by_width<DT, true>(a, s) : ce_by_width<DT, false>(a, s);
 }
-
 hipError_t launch_cross_entropy(const LossArgs& a, int dt, hipStream_t s) {
   if (a.rows == 0) return hipSuccess;
-  if (dt == DT_BF16) return aligned_rows(a, 2) ? ce_by_width<DT_BF16, true>(a, s) : ce_by_width<DT_BF16, false>(a, s);
-  return ce_by_width<DT_F32, false>(a, s);
+  return dt == DT_BF16 ? ce_by_type<DT_BF16>(a, s) : ce_by_type<DT_F32>(a, s);
 }
 
 template <int DT, bool NT>
 static hipError_t lg(LossArgs a, hipStream_t s) {
-  const uint32_t parts = (uint32_t)((((int64_t)a.V + 7) / 8 + LG_OCTETS - 1) / LG_OCTETS);
+  const uint32_t parts = (uint32_t)((row_units<DT>(a) + LG_UNITS - 1) / LG_UNITS);
   const int64_t all = a.rows, most = 4 * MAX_GROUPS / parts;   // V <= 2^30: at least 64
   for (int64_t done = 0; done < all; done += most) {
     a.rows = all - done < most ? all - done : most;
@@ -490,8 +514,8 @@ static hipError_t lg(LossArgs a, hipStream_t s) {
 
 hipError_t launch_logit_grads(const LossArgs& a, int dt, hipStream_t s) {
   if (a.rows == 0) return hipSuccess;
-  if (dt == DT_BF16) return aligned_rows(a, 2) ? lg<DT_BF16, true>(a, s) : lg<DT_BF16, false>(a, s);
-  return lg<DT_F32, false>(a, s);
+  if (dt == DT_BF16) return same_phase<DT_BF16>(a) ? lg<DT_BF16, true>(a, s) : lg<DT_BF16, false>(a, s);
+  return same_phase<DT_F32>(a) ? lg<DT_F32, true>(a, s) : lg<DT_F32, false>(a, s);
 }
 
 hipError_t launch_preference(PreferenceArgs a, int B, hipStream_t s) {

@@ -1,5 +1,5 @@
-// Octets (8 consecutive elements) of rows of any alignment, and sums over the
-// threads that share a row. A part of the sources that include it.
+// Octets (8 consecutive elements) and 16-byte units of rows of any alignment, and sums over
+// the threads that share a row. A part of the sources that include it.
 #pragma once
 #include "common.hpp"
 
@@ -20,32 +20,32 @@ __device__ __forceinline__ u32x4 load16_hint(const char* p) {
   else return load16_any(p);
 }
 
-// An octet's bits as loaded: 16 bytes of bf16, 32 of fp32.
-template <int DT>
+// N consecutive elements' bits as loaded: an octet is 16 bytes of bf16, 32 of fp32.
+template <int DT, int N_ = 8>
 struct Oct {
-  static constexpr int ES = DT == DT_BF16 ? 2 : 4;
-  u32x4 r[DT == DT_BF16 ? 1 : 2];
+  static constexpr int ES = DT == DT_BF16 ? 2 : 4, N = N_, R = N * ES / 16;
+  u32x4 r[R];
 
-  // Elements [0, n) at p (n may be past 8, or not positive: nothing is read); the
-  // others are `fill`, as bits of the type twice in a dword (bf16) or once (fp32).
+  // Elements [lo, n) at p (n may be past N, or not above lo: nothing is read; lo may be below 0);
+  // the others are `fill`, as bits of the type twice in a dword (bf16) or once (fp32).
   template <bool NT = false>
-  __device__ __forceinline__ void load(const char* p, int64_t n, uint32_t fill = 0u) {
-    if (n >= 8) {
-      r[0] = load16_hint<NT>(p);
-      if constexpr (DT == DT_F32) r[1] = load16_hint<NT>(p + 16);
+  __device__ __forceinline__ void load(const char* p, int64_t n, uint32_t fill = 0u, int lo = 0) {
+    if (n >= N && lo <= 0) {
+#pragma unroll
+      for (int q = 0; q < R; ++q) r[q] = load16_hint<NT>(p + 16 * q);
       return;
     }
     if constexpr (DT == DT_BF16) {
       r[0] = u32x4{fill, fill, fill, fill};
 #pragma unroll
-      for (int e = 0; e < 8; ++e)
-        if (e < n) {
+      for (int e = 0; e < N; ++e)
+        if (e < n && e >= lo) {
           const uint32_t v = ((global_u16*)(uintptr_t)p)[e];
           r[0][e >> 1] = (e & 1) ? (r[0][e >> 1] & 0xFFFFu) | (v << 16) : (r[0][e >> 1] & 0xFFFF0000u) | v;
         }
     } else {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) r[e >> 2][e & 3] = e < n ? ((const uint32_t*)p)[e] : fill;
+      for (int e = 0; e < N; ++e) r[e >> 2][e & 3] = e < n && e >= lo ? ((const uint32_t*)p)[e] : fill;
     }
   }
 
@@ -56,28 +56,28 @@ struct Oct {
       return __uint_as_float(r[e >> 2][e & 3]);
   }
 
-  // Rounds eight values to the type (to nearest even; NaN stays NaN).
-  __device__ __forceinline__ void set(const float (&v)[8]) {
+  // Rounds N values to the type (to nearest even; NaN stays NaN).
+  __device__ __forceinline__ void set(const float (&v)[N]) {
     if constexpr (DT == DT_BF16) {
 #pragma unroll
-      for (int q = 0; q < 4; ++q)
+      for (int q = 0; q < N / 2; ++q)
         r[0][q] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{v[2 * q], v[2 * q + 1]}, bf16x2));
     } else {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) r[e >> 2][e & 3] = __float_as_uint(v[e]);
+      for (int e = 0; e < N; ++e) r[e >> 2][e & 3] = __float_as_uint(v[e]);
     }
   }
 
   template <bool NT = false>
-  __device__ __forceinline__ void store(char* p, int64_t n) const {
-    if (n >= 8) {
-      store16_any<NT>(p, r[0]);
-      if constexpr (DT == DT_F32) store16_any<NT>(p + 16, r[1]);
+  __device__ __forceinline__ void store(char* p, int64_t n, int lo = 0) const {
+    if (n >= N && lo <= 0) {
+#pragma unroll
+      for (int q = 0; q < R; ++q) store16_any<NT>(p + 16 * q, r[q]);
       return;
     }
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
-      if (e < n) {
+    for (int e = 0; e < N; ++e)
+      if (e < n && e >= lo) {
         if constexpr (DT == DT_BF16)
           ((uint16_t*)p)[e] = (uint16_t)(r[0][e >> 1] >> ((e & 1) * 16));
         else
@@ -85,6 +85,10 @@ struct Oct {
       }
   }
 };
+
+// A unit: 16 bytes, one access of a lane.
+template <int DT>
+using Unit = Oct<DT, DT == DT_BF16 ? 8 : 4>;
 
 // The sum over a row of 16 lanes, in each of them, by rotating adds (VALU, no LDS
 // permutes): lanes whose values meet add the same two in either order, so all hold the same bits.
