@@ -45,8 +45,10 @@ __device__ __forceinline__ uint16_t* ns_plane(const NsMat& M, int which, int pla
   return (uint16_t*)(M.ws + ns_offset(M.mp, M.np, which, plane, pl));
 }
 
-// Partial sums of squares of G, in double: item = (matrix, part).
-template <int DT>
+// Partial sums of squares of G, in double: item = (matrix, part). Units of 16 bytes, eight in
+// flight. NT: streaming loads, here and in the next kernel, for a group that the
+// memory-side cache does not hold anyway (GPT-2's 340 MB: 57 + 97 us with them, 86 + 82 without).
+template <int DT, bool NT>
 __global__ __launch_bounds__(256) void ns_norm_kernel(NsArgs args) {
   const NsArgs& a = *(const NsArgs*)__builtin_amdgcn_kernarg_segment_ptr();
   (void)args;
@@ -54,15 +56,26 @@ __global__ __launch_bounds__(256) void ns_norm_kernel(NsArgs args) {
   const int ln = (int)(threadIdx.x & (WAVE - 1));
   const int l = wave_find(blockIdx.x, ln < a.n ? a.M[ln].item_begin : 0u, a.n);
   const NsMat& M = a.M[l];
+  constexpr uint32_t N = Unit<DT>::N;
   const uint32_t part = blockIdx.x - M.item_begin, parts = (uint32_t)ns_parts(M.rows, M.cols);
-  const uint32_t per_row = ((uint32_t)M.cols + 7) / 8, total = per_row * (uint32_t)M.rows;
+  // A matrix without gaps is one long row.
+  const bool flat = M.ldg == M.cols;
+  const int cols = flat ? M.rows * M.cols : M.cols;
+  const uint32_t per_row = ((uint32_t)cols + N - 1) / N, total = flat ? per_row : per_row * (uint32_t)M.rows;
+  const uint32_t stride = parts * 256;
+  constexpr int U = 8;   // units in flight
   double sum = 0.0;
-  for (uint32_t o = part * 256 + threadIdx.x; o < total; o += parts * 256) {
-    const uint32_t r = o / per_row, c = (o - r * per_row) * 8;
-    Oct<DT> v;
-    v.load((const char*)M.G + ((int64_t)r * M.ldg + c) * Oct<DT>::ES, M.cols - (int)c);
+  for (uint32_t o = part * 256 + threadIdx.x; o < total; o += U * stride) {
+    Unit<DT> v[U];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) sum = fma((double)v.at(e), (double)v.at(e), sum);
+    for (int u = 0; u < U; ++u) {
+      const uint32_t at = o + u * stride, r = flat ? 0u : at / per_row, c = (at - r * per_row) * N;
+      v[u].template load<NT>((const char*)M.G + ((int64_t)r * M.ldg + c) * Unit<DT>::ES, at < total ? cols - (int)c : 0);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int e = 0; e < (int)N; ++e) sum = fma((double)v[u].at(e), (double)v[u].at(e), sum);
   }
   sum = wave_sum_d(sum);
   if (ln == 0) red[threadIdx.x / WAVE] = sum;
@@ -90,7 +103,7 @@ __device__ __forceinline__ void ns_cut(float (&v)[8], f16x8 (&h)[PL]) {
 }
 
 // Y_0 from G: workgroup = 64 x 64 of the padded Y.
-template <int DT, int PL>
+template <int DT, int PL, bool NT>
 __global__ __launch_bounds__(256) void ns_convert_kernel(NsArgs args) {
   const NsArgs& a = *(const NsArgs*)__builtin_amdgcn_kernarg_segment_ptr();
   (void)args;
@@ -109,7 +122,7 @@ __global__ __launch_bounds__(256) void ns_convert_kernel(NsArgs args) {
 #pragma unroll
   for (int u = 0; u < 2; ++u) {
     const int r = r0 + (tid >> 3) + 32 * u, c = c0 + (tid & 7) * 8;
-    g[u].load((const char*)M.G + ((int64_t)r * M.ldg + c) * Oct<DT>::ES, r < M.rows ? M.cols - c : 0);
+    g[u].template load<NT>((const char*)M.G + ((int64_t)r * M.ldg + c) * Oct<DT>::ES, r < M.rows ? M.cols - c : 0);
   }
   double sq = 0.0;
   for (int p = tid; p < ns_parts(M.rows, M.cols); p += 256) sq += ((const double*)M.ws)[p];
@@ -877,24 +890,31 @@ static hipError_t ns_step(NsArgs& a, const NsBins& bins, hipStream_t s) {
   return ns_launch<PL, NS_UPDATE, 2, FN, false>(a, bins, s);
 }
 
-template <int DT, int PL>
-static hipError_t ns_run(NsArgs a, const float* coef, int steps, hipStream_t s) {
-  const NsBins bins = ns_order(a);
+template <int DT, int PL, bool NT>
+static hipError_t ns_begin(NsArgs& a, hipStream_t s) {
   uint32_t items = 0;
   for (int l = 0; l < a.n; ++l) {
     a.M[l].item_begin = items;
     items += (uint32_t)ns_parts(a.M[l].rows, a.M[l].cols);
   }
-  hipLaunchKernelGGL((ns_norm_kernel<DT>), dim3(items), dim3(256), 0, s, a);
-  hipError_t e = hipGetLastError();
+  hipLaunchKernelGGL((ns_norm_kernel<DT, NT>), dim3(items), dim3(256), 0, s, a);
+  const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   items = 0;
   for (int l = 0; l < a.n; ++l) {
     a.M[l].item_begin = items;
     items += (uint32_t)(a.M[l].mp / 64) * (uint32_t)(a.M[l].np / 64);
   }
-  hipLaunchKernelGGL((ns_convert_kernel<DT, PL>), dim3(items), dim3(256), 0, s, a);
-  e = hipGetLastError();
+  hipLaunchKernelGGL((ns_convert_kernel<DT, PL, NT>), dim3(items), dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+
+template <int DT, int PL>
+static hipError_t ns_run(NsArgs a, const float* coef, int steps, hipStream_t s) {
+  const NsBins bins = ns_order(a);
+  int64_t bytes = 0;
+  for (int l = 0; l < a.n; ++l) bytes += (int64_t)a.M[l].rows * a.M[l].cols * Oct<DT>::ES;
+  hipError_t e = bytes > ((int64_t)256 << 20) ? ns_begin<DT, PL, true>(a, s) : ns_begin<DT, PL, false>(a, s);
   for (int k = 0; k < steps && e == hipSuccess; ++k) {
     for (int q = 0; q < 3; ++q) a.coef[q] = coef[3 * k + q];
     a.step = k;
