@@ -190,6 +190,39 @@ def test_logprobs_and_cross_entropy(dp, dt, B, T, V, pad, off):
     assert torch.equal(z, g)
 
 
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("V", [1, 5, 8, 13, 515, 8200])
+def test_every_alignment_of_logits_and_gradients(dp, dt, V):
+    """Rows that start anywhere in a 16-byte unit, and gradients that start elsewhere in theirs."""
+    B, T, step = 2, 4, 8 if dt == "bf16" else 4
+    x, y = 3 * _normal(V, B, T, V), _targets(B, T, V)
+    y[1, 3] = V - 1
+    w, yd = torch.ones(B, T, device="cuda"), y.cuda()
+    ref = None
+    for off in range(step):
+        z = _rows_of(x, dt, V + 1 + off, off)
+        g = _rows_of(torch.zeros(B, T, V), dt, V + 3, (3 * off + 1) % step)
+        logp = torch.empty(B, T, device="cuda")
+        dp.dp_token_logprobs(z, yd, logp)
+        if ref is None:
+            zs = _host(z)
+            ref = F.token_logprobs(zs, y.numpy()), F.cross_entropy(zs, y.numpy(), np.ones((B, T)))
+        _within(logp, ref[0][0], ref[0][2], "f32", f"offset {off}: logp")
+        dp.dp_cross_entropy(z, yd, w, logp, g)
+        _within(logp, ref[0][0], ref[0][2], "f32", "logp")
+        _within(g, ref[1][1], ref[1][2], dt, "Gz")
+        assert int((g._base == 7).sum()) == (3 * off + 1) % step + B * T * 3
+        h = _rows_of(torch.zeros(B, T, V), dt, V + 2, off)
+        loss = torch.empty(B, device="cuda")
+        dp.dp_preference_loss(z, yd, 2, None, 0.3, loss, Gz=h)
+        want = F.preference(zs, y.numpy(), 2, np.zeros((B, T)), float(np.float32(0.3)), 0.0)
+        _within(h, want["Gz"], want["Gz_error"], dt, "preference Gz")
+        assert int((h._base == 7).sum()) == off + B * T * 2
+        dp.dp_cross_entropy(z, yd, w, None, z)
+        assert int((z._base == 7).sum()) == off + B * T * (1 + off)
+        assert torch.equal(z, g)
+
+
 PAIRS = [("f32", 1, 2, 3, 1, 0), ("bf16", 3, 7, 50, 3, 1), ("f32", 2, 9, 2050, 4, 0),
          ("bf16", 2, 6, 50257, 3, 47), ("f32", 2, 5, 300, 0, 0), ("f32", 2, 5, 300, 5, 2),
          ("bf16", 5, 300, 129, 150, 0)]
