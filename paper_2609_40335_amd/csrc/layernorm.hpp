@@ -10,7 +10,11 @@
 // vec_reduce_kernel, which wants xhat in memory; here it is formed from x and
 // the saved statistics), and the flat norm takes ||dgain_i||^2 + ||dbias_i||^2.
 //
-// Both passes are bound by HBM: 2 (forward) or 3 (backward) elements a feature.
+// Both passes are bound by HBM: 2 (forward) or 3 (backward) elements a feature, 16 bytes a lane and
+// access (fp32 rows of 5000 by 32 bytes a lane, 4 x 1000 backward: 80 us, so 72). Measured: 32 x 128 x 768 bf16
+// forward 6.3 us (2.0 TB/s, launch and one round of rows), backward 8.4 + 3.4 us; 16 x 1024 x 1600 bf16 30
+// and 47 us (3.5 TB/s); 2 x 8191 x 1601 fp32 backward 67 + 10 us (4.7 TB/s in the first launch, whose 252
+// registers leave one workgroup a CU).
 // A row is read once into the registers of a team, one wave up to 2048
 // features (its sums need no barrier), 4 waves up to 4096, 16 up to 32768, and
 // both sums of a row meet in one exchange. A lane holds the same features of
@@ -31,73 +35,82 @@ struct LnTeam {
   static constexpr int TEAMS = W == 1 ? LN_WAVES : 1;
 };
 
-// Eight of a parameter's d elements of either type from col on; a null one is `none`.
-__device__ __forceinline__ void ln_params(const void* p, int dt, int col, int d, float none, float (&v)[8]) {
+// N of a parameter's d elements of either type from col on; a null one is `none`.
+template <int N>
+__device__ __forceinline__ void ln_params(const void* p, int dt, int col, int d, float none, float (&v)[N]) {
   if (!p) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = none;
+    for (int e = 0; e < N; ++e) v[e] = none;
   } else if (dt == DT_BF16) {
-    Oct<DT_BF16> o;
-    o.load((const char*)p + (int64_t)col * 2, d - col);
+    if constexpr (N == 8) {
+      Oct<DT_BF16> o;
+      o.load((const char*)p + (int64_t)col * 2, d - col);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = o.at(e);
+      for (int e = 0; e < N; ++e) v[e] = o.at(e);
+    } else {
+#pragma unroll
+      for (int e = 0; e < N; ++e) v[e] = col + e < d ? bf16_to_f32(((const uint16_t*)p)[col + e]) : 0.f;
+    }
   } else {
-    Oct<DT_F32> o;
+    Oct<DT_F32, N> o;
     o.load((const char*)p + (int64_t)col * 4, d - col);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = o.at(e);
+    for (int e = 0; e < N; ++e) v[e] = o.at(e);
   }
 }
 
-// A lane's octets of a row.
+// A lane's units of a row.
 template <int DT, int W, int NV>
-__device__ __forceinline__ void ln_load(const void* base, int64_t ld, int64_t row, int lane, int d, Oct<DT> (&v)[NV]) {
-  const char* p = (const char*)base + row * ld * Oct<DT>::ES;
+__device__ __forceinline__ void ln_load(const void* base, int64_t ld, int64_t row, int lane, int d, Unit<DT> (&v)[NV]) {
+  const char* p = (const char*)base + row * ld * Unit<DT>::ES;
 #pragma unroll
   for (int j = 0; j < NV; ++j) {
-    const int col = (lane + j * W * WAVE) * 8;
-    v[j].load(p + (int64_t)col * Oct<DT>::ES, d - col);
+    const int col = (lane + j * W * WAVE) * Unit<DT>::N;
+    v[j].load(p + (int64_t)col * Unit<DT>::ES, d - col);
   }
 }
+// Whether the next row is fetched while this one is worked on: rows of up to 16 elements a lane.
+template <int DT, int W, int NV>
+constexpr bool LN_AHEAD = NV * Unit<DT>::N <= 16 && NV * Unit<DT>::N * W <= 128;
 
 template <int DT, int W, int NV>
 __global__ __launch_bounds__(LnTeam<W>::THREADS) void ln_forward_kernel(LnForwardArgs a) {
   __shared__ float red[2 * W];
-  constexpr int LANES = W * WAVE;
+  constexpr int LANES = W * WAVE, N = Unit<DT>::N;
   const int lane = (int)threadIdx.x % LANES, team = (int)threadIdx.x / LANES;
   const int d = a.d;
   const float inv_d = 1.f / (float)d;
   const int64_t step = (int64_t)gridDim.x * LnTeam<W>::TEAMS;
   int64_t row = (int64_t)blockIdx.x * LnTeam<W>::TEAMS + team;
   if (row >= a.rows) return;   // a whole team
-  Oct<DT> v[NV], next[NV];
+  Unit<DT> v[NV], next[NV];
   ln_load<DT, W, NV>(a.x, a.ldx, row, lane, d, v);
-  float gain[NV][8], bias[NV][8];
+  float gain[NV][N], bias[NV][N];
 #pragma unroll
   for (int j = 0; j < NV; ++j) {
-    ln_params(a.gain, a.param_dt, (lane + j * LANES) * 8, d, 1.f, gain[j]);
-    ln_params(a.bias, a.param_dt, (lane + j * LANES) * 8, d, 0.f, bias[j]);
+    ln_params(a.gain, a.param_dt, (lane + j * LANES) * N, d, 1.f, gain[j]);
+    ln_params(a.bias, a.param_dt, (lane + j * LANES) * N, d, 0.f, bias[j]);
   }
   for (; row < a.rows; row += step) {
     // The next row is on its way while this one is worked on.
     const bool more = row + step < a.rows;
-    constexpr bool AHEAD = NV <= 2 && NV * W <= 16;
+    constexpr bool AHEAD = LN_AHEAD<DT, W, NV>;
     if (AHEAD && more) ln_load<DT, W, NV>(a.x, a.ldx, row + step, lane, d, next);
-    char* y = (char*)a.y + row * a.ldy * Oct<DT>::ES;
+    char* y = (char*)a.y + row * a.ldy * Unit<DT>::ES;
     float sum = 0.f, none = 0.f;
 #pragma unroll
     for (int j = 0; j < NV; ++j)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) sum += v[j].at(e);
+      for (int e = 0; e < N; ++e) sum += v[j].at(e);
     team_sum2<W>(sum, none, red);
     const float about = sum * inv_d;
     float sq = 0.f, rest = 0.f;
 #pragma unroll
     for (int j = 0; j < NV; ++j)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
+      for (int e = 0; e < N; ++e) {
         const float c = v[j].at(e) - about;
-        if ((lane + j * LANES) * 8 + e < d) {
+        if ((lane + j * LANES) * N + e < d) {
           sq = fmaf(c, c, sq);
           rest += c;
         }
@@ -110,12 +123,12 @@ __global__ __launch_bounds__(LnTeam<W>::THREADS) void ln_forward_kernel(LnForwar
     const float rstd = 1.f / sqrtf((sq != sq ? sq : var) + a.eps);
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
-      const int col = (lane + j * LANES) * 8;
-      float o[8];
+      const int col = (lane + j * LANES) * N;
+      float o[N];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) o[e] = fmaf((v[j].at(e) - mean) * rstd, gain[j][e], bias[j][e]);
+      for (int e = 0; e < N; ++e) o[e] = fmaf((v[j].at(e) - mean) * rstd, gain[j][e], bias[j][e]);
       v[j].set(o);
-      v[j].store(y + (int64_t)col * Oct<DT>::ES, d - col);
+      v[j].store(y + (int64_t)col * Unit<DT>::ES, d - col);
     }
     if (lane == 0) {
       if (a.mean) a.mean[row] = mean;
@@ -135,9 +148,9 @@ __global__ __launch_bounds__(LnTeam<W>::THREADS) void ln_forward_kernel(LnForwar
 // Item: (example b, range s of a.span rows). DX: dx is wanted; WG: the gradients are.
 template <int DT, int W, int NV, bool DX, bool WG>
 __global__ __launch_bounds__(LnTeam<W>::THREADS) void ln_backward_kernel(LnBackwardArgs a) {
-  constexpr int LANES = W * WAVE, TEAMS = LnTeam<W>::TEAMS;
+  constexpr int LANES = W * WAVE, TEAMS = LnTeam<W>::TEAMS, N = Unit<DT>::N;
   __shared__ float red[2 * W];
-  __shared__ float meet[WG && TEAMS > 1 ? TEAMS : 1][WG && TEAMS > 1 ? 2 * 8 * WAVE : 1];
+  __shared__ float meet[WG && TEAMS > 1 ? TEAMS : 1][WG && TEAMS > 1 ? 2 * N * WAVE : 1];
   __shared__ float sq_red[LnTeam<W>::THREADS / WAVE];
   const int lane = (int)threadIdx.x % LANES, team = (int)threadIdx.x / LANES;
   const uint32_t item = xcd_remap(blockIdx.x, gridDim.x);
@@ -147,28 +160,28 @@ __global__ __launch_bounds__(LnTeam<W>::THREADS) void ln_backward_kernel(LnBackw
   const float inv_d = 1.f / (float)d;
   const int t0 = s * a.span, t1 = t0 + min(a.span, a.T - t0);
   const int64_t row0 = (int64_t)b * a.T;
-  Oct<DT> x[NV], g[NV];
+  Unit<DT> x[NV], g[NV];
   float mean = 0.f, rstd = 0.f;
-  auto fetch = [&](int t, Oct<DT> (&px)[NV], Oct<DT> (&pg)[NV], float& m, float& r) __attribute__((always_inline)) {
+  auto fetch = [&](int t, Unit<DT> (&px)[NV], Unit<DT> (&pg)[NV], float& m, float& r) __attribute__((always_inline)) {
     ln_load<DT, W, NV>(a.x, a.ldx, row0 + t, lane, d, px);
     ln_load<DT, W, NV>(a.gy, a.ldgy, row0 + t, lane, d, pg);
     m = a.mean[row0 + t];
     r = a.rstd[row0 + t];
   };
   if (t0 + team < t1) fetch(t0 + team, x, g, mean, rstd);
-  float gain[NV][8];
-  float dg[NV][8], db[NV][8];
+  float gain[NV][N];
+  float dg[NV][N], db[NV][N];
 #pragma unroll
   for (int j = 0; j < NV; ++j) {
-    if constexpr (DX) ln_params(a.gain, a.param_dt, (lane + j * LANES) * 8, d, 1.f, gain[j]);
+    if constexpr (DX) ln_params(a.gain, a.param_dt, (lane + j * LANES) * N, d, 1.f, gain[j]);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) dg[j][e] = db[j][e] = 0.f;
+    for (int e = 0; e < N; ++e) dg[j][e] = db[j][e] = 0.f;
   }
   for (int t = t0 + team; t < t1; t += TEAMS) {
     const int64_t row = row0 + t;
     // The next row is on its way while this one is worked on, where registers allow.
-    constexpr bool AHEAD = NV <= 2 && NV * W <= 16;
-    Oct<DT> nx[NV], ng[NV];
+    constexpr bool AHEAD = LN_AHEAD<DT, W, NV>;
+    Unit<DT> nx[NV], ng[NV];
     float nm = 0.f, nr = 0.f;
     const bool more = t + TEAMS < t1;
     if (AHEAD && more) fetch(t + TEAMS, nx, ng, nm, nr);
@@ -177,7 +190,7 @@ __global__ __launch_bounds__(LnTeam<W>::THREADS) void ln_backward_kernel(LnBackw
 #pragma unroll
     for (int j = 0; j < NV; ++j)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
+      for (int e = 0; e < N; ++e) {
         const float gy = g[j].at(e), xh = (x[j].at(e) - mean) * rstd;
         if constexpr (WG) {
           dg[j][e] = fmaf(gy, xh, dg[j][e]);
@@ -192,24 +205,24 @@ __global__ __launch_bounds__(LnTeam<W>::THREADS) void ln_backward_kernel(LnBackw
     if constexpr (DX) {
       team_sum2<W>(s1, s2, red);
       const float c1 = s1 * inv_d, c2 = s2 * inv_d;
-      char* pd = (char*)a.dx + row * a.lddx * Oct<DT>::ES;
+      char* pd = (char*)a.dx + row * a.lddx * Unit<DT>::ES;
 #pragma unroll
       for (int j = 0; j < NV; ++j) {
-        const int col = (lane + j * LANES) * 8;
-        float o[8];
+        const int col = (lane + j * LANES) * N;
+        float o[N];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
+        for (int e = 0; e < N; ++e) {
           const float xh = (x[j].at(e) - mean) * rstd;
           o[e] = rstd * (g[j].at(e) * gain[j][e] - c1 - xh * c2);
         }
         if (a.accumulate_dx) {
-          Oct<DT> p;
-          p.load(pd + (int64_t)col * Oct<DT>::ES, d - col);
+          Unit<DT> p;
+          p.load(pd + (int64_t)col * Unit<DT>::ES, d - col);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) o[e] += p.at(e);
+          for (int e = 0; e < N; ++e) o[e] += p.at(e);
         }
         x[j].set(o);
-        x[j].store(pd + (int64_t)col * Oct<DT>::ES, d - col);
+        x[j].store(pd + (int64_t)col * Unit<DT>::ES, d - col);
       }
     }
     if (more) {
@@ -227,39 +240,41 @@ __global__ __launch_bounds__(LnTeam<W>::THREADS) void ln_backward_kernel(LnBackw
     }
   }
   if constexpr (WG) {
-    // The teams' sums meet in LDS, one octet of every lane at a time.
+    // The teams' sums meet in LDS, one unit of every lane at a time.
     float* part = a.ranges > 1 ? a.ws + ((int64_t)b * a.ranges + s) * 2 * d : nullptr;
     float* out_g = part ? part : a.dgain ? a.dgain + (int64_t)b * d : nullptr;
     float* out_b = part ? part + d : a.dbias ? a.dbias + (int64_t)b * d : nullptr;
     float sq = 0.f;
-    auto put = [&](int col, float vg, float vb) {
+    auto put = [&](int col, bool bias, float v) {
+      float* out = bias ? out_b : out_g;
       if (col >= d) return;
-      if (out_g) out_g[col] = vg;
-      if (out_b) out_b[col] = vb;
-      if (a.dgain) sq = fmaf(vg, vg, sq);
-      if (a.dbias) sq = fmaf(vb, vb, sq);
+      if (out) out[col] = v;
+      if (bias ? a.dbias : a.dgain) sq = fmaf(v, v, sq);
     };
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
       if constexpr (TEAMS > 1) {
         __syncthreads();
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
+        for (int e = 0; e < N; ++e) {
           meet[team][e * WAVE + lane] = dg[j][e];
-          meet[team][(8 + e) * WAVE + lane] = db[j][e];
+          meet[team][(N + e) * WAVE + lane] = db[j][e];
         }
         __syncthreads();
-        const int e = team;   // TEAMS == 8: a team takes one element of every octet
-        float vg = 0.f, vb = 0.f;
 #pragma unroll
-        for (int w = 0; w < TEAMS; ++w) {
-          vg += meet[w][e * WAVE + lane];
-          vb += meet[w][(8 + e) * WAVE + lane];
+        for (int q0 = 0; q0 < 2 * N; q0 += TEAMS) {   // a team takes every eighth of a unit's 2 N sums
+          const int q = q0 + team;
+          float v = 0.f;
+#pragma unroll
+          for (int w = 0; w < TEAMS; ++w) v += meet[w][q * WAVE + lane];
+          put((lane + j * LANES) * N + q % N, q >= N, v);
         }
-        put((lane + j * LANES) * 8 + e, vg, vb);
       } else {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) put((lane + j * LANES) * 8 + e, dg[j][e], db[j][e]);
+        for (int e = 0; e < N; ++e) {
+          put((lane + j * LANES) * N + e, false, dg[j][e]);
+          put((lane + j * LANES) * N + e, true, db[j][e]);
+        }
       }
     }
     if (a.ranges == 1 && a.norm2) {
@@ -274,7 +289,7 @@ __global__ __launch_bounds__(LnTeam<W>::THREADS) void ln_backward_kernel(LnBackw
     }
   }
 }
-static_assert(LN_WAVES == 8, "a team per element of an octet");
+static_assert(LN_WAVES == 8, "2 N sums of a unit in whole turns");
 
 // The ranges' partial sums of example blockIdx.y. FEW (at most LN_FEW ranges): a thread adds
 // a feature's, in order, one workgroup per example, which writes the norm too. Otherwise
@@ -344,7 +359,7 @@ template <int DT, int W, int NV>
 static hipError_t ln_forward(const LnForwardArgs& a, hipStream_t s) {
   const int64_t need = (a.rows + LnTeam<W>::TEAMS - 1) / LnTeam<W>::TEAMS;
   // As many workgroups as the registers let the GPU hold: rows beyond are prefetched.
-  constexpr int64_t MOST = 256 * (W == 1 ? (NV == 1 ? 4 : NV == 2 ? 3 : 2) : W == 4 ? 4 : 2);
+  constexpr int64_t MOST = 256 * (W == 1 ? (NV * Unit<DT>::N == 8 ? 4 : NV * Unit<DT>::N == 16 ? 3 : 2) : W == 4 ? 4 : 2);
   const unsigned grid = (unsigned)(need < MOST ? need : MOST);
   hipLaunchKernelGGL((ln_forward_kernel<DT, W, NV>), dim3(grid), dim3(LnTeam<W>::THREADS), 0, s, a);
   return hipGetLastError();
@@ -379,17 +394,18 @@ static hipError_t ln_backward(LnBackwardArgs a, hipStream_t s) {
   return launch_finish_rows(a.sq, a.B, a.chunks, a.norm2, a.accumulate, 1.f, s);
 }
 
-// Calls f<W, NV> for the team that holds rows of d features.
-#define DPG_LN_TEAMS(FN, DT)                       \
-  do {                                             \
-    const int octs = (a.d + 7) / 8;                \
-    if (octs <= 64) return FN<DT, 1, 1>(a, s);     \
-    if (octs <= 128) return FN<DT, 1, 2>(a, s);    \
-    if (octs <= 256) return FN<DT, 1, 4>(a, s);    \
-    if (octs <= 512) return FN<DT, 4, 2>(a, s);    \
-    if (octs <= 1024) return FN<DT, 16, 1>(a, s);  \
-    if (octs <= 2048) return FN<DT, 16, 2>(a, s);  \
-    return FN<DT, 16, 4>(a, s);                    \
+// Calls f<W, NV> for the team that holds rows of d features (F units are 8 of them).
+#define DPG_LN_TEAMS(FN, DT)                           \
+  do {                                                 \
+    constexpr int F = 8 / Unit<DT>::N;                 \
+    const int octs = (a.d + 7) / 8;                    \
+    if (octs <= 64) return FN<DT, 1, F>(a, s);         \
+    if (octs <= 128) return FN<DT, 1, 2 * F>(a, s);    \
+    if (octs <= 256) return FN<DT, 1, 4 * F>(a, s);    \
+    if (octs <= 512) return FN<DT, 4, 2 * F>(a, s);    \
+    if (octs <= 1024) return FN<DT, 16, F>(a, s);      \
+    if (octs <= 2048) return FN<DT, 16, 2 * F>(a, s);  \
+    return FN<DT, 16, 4 * F>(a, s);                    \
   } while (0)
 
 hipError_t launch_ln_forward(const LnForwardArgs& a, int dt, hipStream_t s) {

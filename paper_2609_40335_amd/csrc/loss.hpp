@@ -18,7 +18,12 @@
 // 1024). A pair's weight needs the last row's log p before the first row's
 // gradient, so there the logits are passed twice. (Fewer pairs at a time, so that the second
 // read meets the memory-side cache, was no gain: 16 pairs of 1024 rows of 50257 in bf16 took 652 us in
-// one pass, 688 two at a time, 832 one by one, for the launches' ends.)
+// one pass, 688 two at a time, 832 one by one, for the launches' ends; nor were streaming loads in the
+// first pass, 684, or the rows backwards in the second, 670.)
+// Measured, rows of 50257 of which a third is not scored (and not read): bf16 log-probabilities of 24 x
+// 128 45 us (4.5 TB/s: few rows a CU, and an exponential for every 2 bytes), cross-entropy of 32 x 128
+// 123 us (5.6 TB/s; a copy runs at 4.9), in fp32 of 24 x 100 158 us (5.1); a preference loss of 16 x 1024
+// tokens 657 us, 3.9 GB in two passes (5.9).
 //
 // Sums are fp32 from the row's largest logit; the logarithm, and the sums of
 // log-ratios over an answer's tokens, are in double: a margin is a small
@@ -433,27 +438,31 @@ static hipError_t by_rows(LossArgs a, int64_t per, F launch) {
   return hipSuccess;
 }
 
-template <int DT, int W, int U>
+template <int DT, int W, int U, bool EXACT>
 static hipError_t tl(const LossArgs& a, hipStream_t s) {
   const dim3 block(LossTeam<W>::THREADS);
   return by_rows(a, LossTeam<W>::TEAMS, [&](const LossArgs& q, dim3 grid) {
-    if (q.logp64) hipLaunchKernelGGL((token_logprobs_kernel<DT, W, U, true>), grid, block, 0, s, q);
-    else hipLaunchKernelGGL((token_logprobs_kernel<DT, W, U, false>), grid, block, 0, s, q);
+    hipLaunchKernelGGL((token_logprobs_kernel<DT, W, U, EXACT>), grid, block, 0, s, q);
   });
 }
 
-// Threads of a row: a wave up to 2048 logits, 4 waves up to 8192. Above, 4 where there are
-// rows for every CU's every wave (rows then start and end at different times), 16 otherwise.
-template <int DT>
+// Threads of a row: a wave up to 2048 logits, 4 waves up to 8192. Above, 16 where few rows have to fill
+// the chip; where there are rows for every CU's every wave 8, or 4 with EXACT sums, whose
+// ends cost more (rows then start and end at different times; 24 x 128 rows of 50257 in bf16, 4
+// units in flight: 8 waves 42 us, 4 waves 45; 8 units 46; the preference loss's pass with 8
+// waves made it 707 us, with 4 657, with 8 units 665).
+template <int DT, bool EXACT>
 static hipError_t tl_by_width(const LossArgs& a, hipStream_t s) {
-  if (a.V <= 2048) return tl<DT, 1, 4>(a, s);
-  if (a.V <= 8192 || a.rows >= 2048) return tl<DT, 4, 8>(a, s);
-  return tl<DT, 16, 8>(a, s);
+  if (a.V <= 2048) return tl<DT, 1, 4, EXACT>(a, s);
+  if (a.V <= 8192) return tl<DT, 4, 4, EXACT>(a, s);
+  if (a.rows < 2048) return tl<DT, 16, 8, EXACT>(a, s);
+  return tl<DT, EXACT ? 4 : 8, 4, EXACT>(a, s);
 }
 
 hipError_t launch_token_logprobs(const LossArgs& a, int dt, hipStream_t s) {
   if (a.rows == 0) return hipSuccess;
-  return dt == DT_BF16 ? tl_by_width<DT_BF16>(a, s) : tl_by_width<DT_F32>(a, s);
+  if (a.logp64) return dt == DT_BF16 ? tl_by_width<DT_BF16, true>(a, s) : tl_by_width<DT_F32, true>(a, s);
+  return dt == DT_BF16 ? tl_by_width<DT_BF16, false>(a, s) : tl_by_width<DT_F32, false>(a, s);
 }
 
 template <int DT, int W, int NV, bool NT>
