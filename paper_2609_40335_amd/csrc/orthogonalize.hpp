@@ -5,7 +5,10 @@
 //   A = X X^T,  P = a I + b A + c A^2,  X <- P X        (once per step)
 // and out = (prior) + scale X. A and A^2 are symmetric: only tiles on and above
 // the diagonal are computed, and stored twice. So a step costs
-// m(m+1)n + m^2(m+1) + 2 m^2 n operations in three launches for the whole group.
+// m(m+1)n + m^2(m+1) + 2 m^2 n operations in three launches for the whole group. Bound by the
+// matrix cores: GPT-2's 48 block matrices 98 us for A, 43 for A^2 and 163 for the update (800
+// TFLOP/s), 1.6 ms in five steps; 1601 x 6397 with two planes 104 us an update (950 TFLOP/s of fp16
+// products), 1.04 ms in five steps.
 //
 // The products run on the fp16 matrix cores. Singular values are at most about
 // 1.2 on the way, so that X, held as 2^12 X, and A and P, held as 2^10 A and
@@ -620,8 +623,9 @@ __global__ __launch_bounds__(256) void ns_join_kernel(NsArgs args) {
 // All steps of a matrix in one workgroup, its Y, A and P in LDS as the buffers' blocks (see
 // above; sides padded to 32, blocks along mp). A wave takes every eighth 32 x 32 block
 // of a product. An update's blocks stay in registers until every wave has read Y.
-// (Four matrices of a block of width 64, five steps, fp32 results: 17 launches of 5 to 9 us
-// each took 143 us.)
+// Bound by latency: fifteen products in a row, each a barrier, a chain of LDS reads and the turn
+// through the slice. (Four matrices of a block of width 64, five steps, fp32 results: 41 us; in 17
+// launches of 5 to 9 us each 143.)
 template <int DT, int PL>
 __global__ __launch_bounds__(NS_SMALL_WAVES * WAVE) void ns_small_kernel(NsArgs args, NsCoefs coefs) {
   const NsArgs& a = *(const NsArgs*)__builtin_amdgcn_kernarg_segment_ptr();
@@ -807,7 +811,7 @@ static uint32_t ns_tiles(const NsMat& M) {
 // of the list (neighbouring tiles share operand panels through its L2), whole
 // matrices where ns_order's bins are even for this product, equal work otherwise. (In the
 // caller's order, with equal counts, the Gram of GPT-2's blocks took 128 us: the XCDs
-// of the longest sums were last. So dealt it takes 105.)
+// of the longest sums were last. So dealt it takes 98 to 105.)
 template <int PL, int KIND, int FM, int FN, bool PART>
 static hipError_t ns_launch(NsArgs& a, const NsBins& bins, hipStream_t s) {
   uint32_t items = 0;
