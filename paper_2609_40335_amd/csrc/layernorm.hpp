@@ -11,10 +11,10 @@
 // the saved statistics), and the flat norm takes ||dgain_i||^2 + ||dbias_i||^2.
 //
 // Both passes are bound by HBM: 2 (forward) or 3 (backward) elements a feature, 16 bytes a lane and
-// access (fp32 rows of 5000 by 32 bytes a lane, 4 x 1000 backward: 80 us, so 72). Measured: 32 x 128 x 768 bf16
-// forward 6.3 us (2.0 TB/s, launch and one round of rows), backward 8.4 + 3.4 us; 16 x 1024 x 1600 bf16 30
-// and 47 us (3.5 TB/s); 2 x 8191 x 1601 fp32 backward 67 + 10 us (4.7 TB/s in the first launch, whose 252
-// registers leave one workgroup a CU).
+// access (fp32 rows of 5000 by 32 bytes a lane, 4 x 1000 backward: 80 us, so 72). Measured: 32 x 128 x 768
+// bf16 forward 6.3 us (2.0 TB/s, launch and one round of rows), backward 8.4 + 3.4 us; 16 x 1024 x 1600
+// bf16 30 and 47 us (3.5 TB/s), 32 x 1024 x 768 backward 40 (3.8); 2 x 8191 x 1601 fp32 backward 67 + 10
+// us (4.7 TB/s in the first launch, whose 252 registers leave one workgroup a CU).
 // A row is read once into the registers of a team, one wave up to 2048
 // features (its sums need no barrier), 4 waves up to 4096, 16 up to 32768, and
 // both sums of a row meet in one exchange. A lane holds the same features of
@@ -145,6 +145,13 @@ __global__ __launch_bounds__(LnTeam<W>::THREADS) void ln_forward_kernel(LnForwar
   }
 }
 
+// Rows of 513 to 1024 features: values that the second pass over a row could use again, and second
+// copies of the running sums, are not kept in registers, so that two workgroups fit a CU instead of one
+// (fp32 then without the next row; 32 x 1024 x 768 bf16 42.5 us, so 39.9; 32 x 512 x 768 fp32 39.0,
+// 36.8). Elsewhere it only costs (16 x 1024 x 1600 bf16 47.3 and 48.4).
+template <int DT, int W, int NV>
+constexpr bool LN_LEAN = W == 1 && NV * Unit<DT>::N == 16;
+
 // Item: (example b, range s of a.span rows). DX: dx is wanted; WG: the gradients are.
 template <int DT, int W, int NV, bool DX, bool WG>
 __global__ __launch_bounds__(LnTeam<W>::THREADS) void ln_backward_kernel(LnBackwardArgs a) {
@@ -180,7 +187,7 @@ __global__ __launch_bounds__(LnTeam<W>::THREADS) void ln_backward_kernel(LnBackw
   for (int t = t0 + team; t < t1; t += TEAMS) {
     const int64_t row = row0 + t;
     // The next row is on its way while this one is worked on, where registers allow.
-    constexpr bool AHEAD = LN_AHEAD<DT, W, NV>;
+    constexpr bool LEAN = LN_LEAN<DT, W, NV>, AHEAD = LN_AHEAD<DT, W, NV> && !(LEAN && WG && DT == DT_F32);
     Unit<DT> nx[NV], ng[NV];
     float nm = 0.f, nr = 0.f;
     const bool more = t + TEAMS < t1;
@@ -195,6 +202,7 @@ __global__ __launch_bounds__(LnTeam<W>::THREADS) void ln_backward_kernel(LnBackw
         if constexpr (WG) {
           dg[j][e] = fmaf(gy, xh, dg[j][e]);
           db[j][e] += gy;
+          if constexpr (LEAN) asm volatile("" : "+v"(dg[j][e]), "+v"(db[j][e]));
         }
         if constexpr (DX) {
           const float w = gy * gain[j][e];
@@ -204,6 +212,10 @@ __global__ __launch_bounds__(LnTeam<W>::THREADS) void ln_backward_kernel(LnBackw
       }
     if constexpr (DX) {
       team_sum2<W>(s1, s2, red);
+      if constexpr (LEAN) {   // without the gradients too, so that dx has the same bits
+#pragma unroll
+        for (int j = 0; j < NV; ++j) asm volatile("" : "+v"(x[j].r[0]), "+v"(g[j].r[0]));
+      }
       const float c1 = s1 * inv_d, c2 = s2 * inv_d;
       char* pd = (char*)a.dx + row * a.lddx * Unit<DT>::ES;
 #pragma unroll
