@@ -251,9 +251,11 @@ __device__ __forceinline__ void zero_row(char* g, int V, int lane, int lanes) {
 // that are read again for the gradient. Loads are streaming ones, and stores where their
 // units are aligned too (NT) (32 x 128 bf16 rows of 50257: 140 us without the hints, 129 with).
 // (Eight waves a SIMD: a CU then works on two rows of 16 waves, one loading while the other
-// computes.)
+// computes. Longer rows, up to 24 units a lane, have a CU to themselves, which still beats reading them
+// twice: 1024 bf16 rows of 65000 54 us, read twice 75; of 131072 117 and 138; of 170000 173, 4.0 TB/s, where rows
+// read twice reach 3.4.)
 template <int DT, int W, int NV, bool NT>
-__global__ __launch_bounds__(LossTeam<W>::THREADS, DT == DT_BF16 ? 8 : 4) void cross_entropy_kernel(LossArgs a) {
+__global__ __launch_bounds__(LossTeam<W>::THREADS, DT == DT_BF16 && NV <= 8 ? 8 : 4) void cross_entropy_kernel(LossArgs a) {
   __shared__ double red[2 * W];
   __shared__ float zt_s[LossTeam<W>::TEAMS];
   constexpr int LANES = W * WAVE, ES = Unit<DT>::ES, N = Unit<DT>::N;
@@ -494,6 +496,9 @@ static hipError_t ce_by_width(const LossArgs& a, hipStream_t s) {
   if (units <= 1024 * F) return ce<DT, 4, 4 * F, NT>(a, s);
   if (units <= 4096 * F) return ce<DT, 16, 4 * F, NT>(a, s);
   if (units <= 7168 * F) return ce<DT, 16, 7 * F, NT>(a, s);
+  if (DT == DT_BF16 && units <= 8192) return ce<DT, 16, 8, NT>(a, s);
+  if (units <= 16384) return ce<DT, 16, 16, NT>(a, s);
+  if (units <= 24576) return ce<DT, 16, 24, NT>(a, s);
   return ce<DT, 16, 0, NT>(a, s);
 }
 

@@ -161,6 +161,8 @@ LOSS = [
     ("f32", 2, 4, 8193, 0, 1), ("bf16", 2, 6, 32768, 0, 0), ("f32", 1, 6, 40001, 0, 0),
     ("bf16", 2, 10, 50257, 0, 0), ("f32", 1, 6, 50257, 47, 0), ("bf16", 1, 6, 65537, 0, 0),
     ("f32", 1, 6, 131075, 1, 0), ("bf16", 40, 60, 96, 0, 0),
+    ("bf16", 1, 6, 60001, 0, 1), ("bf16", 1, 6, 131072, 0, 0), ("bf16", 1, 6, 150001, 2, 0),
+    ("bf16", 1, 6, 196609, 0, 0), ("f32", 1, 6, 60001, 0, 0), ("f32", 1, 6, 98304, 8, 0),
 ]
 
 
