@@ -148,9 +148,14 @@ __global__ __launch_bounds__(LnTeam<W>::THREADS) void ln_forward_kernel(LnForwar
 // Rows of 513 to 1024 features: values that the second pass over a row could use again, and second
 // copies of the running sums, are not kept in registers, so that two workgroups fit a CU instead of one
 // (fp32 then without the next row; 32 x 1024 x 768 bf16 42.5 us, so 39.9; 32 x 512 x 768 fp32 39.0,
-// 36.8). Elsewhere it only costs (16 x 1024 x 1600 bf16 47.3 and 48.4).
+// 36.8); nor are those of more than 4096, whose 16 waves leave each lane 128 registers (8 x 512 x 12288 bf16 117,
+// 103). Elsewhere it only costs (16 x 1024 x 1600 bf16 47.3 and 48.4).
 template <int DT, int W, int NV>
-constexpr bool LN_LEAN = W == 1 && NV * Unit<DT>::N == 16;
+constexpr bool LN_LEAN = W == 1 ? NV * Unit<DT>::N == 16 : W == 16;
+// Rows of more than 16384 features: the gain waits in LDS (8 x 512 x 20480 bf16 233 us, 780 with all of it in
+// registers, most of them spilled; 2 x 1024 x 20480 fp32 233 and 319).
+template <int DT, int W, int NV>
+constexpr bool LN_GAIN_LDS = W == 16 && NV * Unit<DT>::N == 32;
 
 // Item: (example b, range s of a.span rows). DX: dx is wanted; WG: the gradients are.
 template <int DT, int W, int NV, bool DX, bool WG>
@@ -176,11 +181,21 @@ __global__ __launch_bounds__(LnTeam<W>::THREADS) void ln_backward_kernel(LnBackw
     r = a.rstd[row0 + t];
   };
   if (t0 + team < t1) fetch(t0 + team, x, g, mean, rstd);
-  float gain[NV][N];
+  constexpr bool GL = LN_GAIN_LDS<DT, W, NV> && DX;
+  __shared__ float gain_s[GL ? NV * N * LANES : 1];   // a lane reads what it wrote
+  float gain[GL ? 1 : NV][N];
+  auto gain_of = [&](int j, int e) __attribute__((always_inline)) {
+    if constexpr (GL) return gain_s[(j * N + e) * LANES + lane];
+    else return gain[j][e];
+  };
   float dg[NV][N], db[NV][N];
 #pragma unroll
   for (int j = 0; j < NV; ++j) {
-    if constexpr (DX) ln_params(a.gain, a.param_dt, (lane + j * LANES) * N, d, 1.f, gain[j]);
+    if constexpr (DX) ln_params(a.gain, a.param_dt, (lane + j * LANES) * N, d, 1.f, gain[GL ? 0 : j]);
+    if constexpr (GL) {
+#pragma unroll
+      for (int e = 0; e < N; ++e) gain_s[(j * N + e) * LANES + lane] = gain[0][e];
+    }
 #pragma unroll
     for (int e = 0; e < N; ++e) dg[j][e] = db[j][e] = 0.f;
   }
@@ -205,7 +220,7 @@ __global__ __launch_bounds__(LnTeam<W>::THREADS) void ln_backward_kernel(LnBackw
           if constexpr (LEAN) asm volatile("" : "+v"(dg[j][e]), "+v"(db[j][e]));
         }
         if constexpr (DX) {
-          const float w = gy * gain[j][e];
+          const float w = gy * gain_of(j, e);
           s1 += w;
           s2 = fmaf(w, xh, s2);
         }
@@ -225,7 +240,7 @@ __global__ __launch_bounds__(LnTeam<W>::THREADS) void ln_backward_kernel(LnBackw
 #pragma unroll
         for (int e = 0; e < N; ++e) {
           const float xh = (x[j].at(e) - mean) * rstd;
-          o[e] = rstd * (g[j].at(e) * gain[j][e] - c1 - xh * c2);
+          o[e] = rstd * (g[j].at(e) * gain_of(j, e) - c1 - xh * c2);
         }
         if (a.accumulate_dx) {
           Unit<DT> p;
