@@ -601,18 +601,23 @@ dp_status_t dp_preference_loss(const void* Z, int64_t ldz, const int32_t* target
  * coef is a host array of steps * 3 floats (a_k, b_k, c_k); eps > 0 keeps a
  * zero matrix zero (eps = 0 is allowed). With accumulate, scale = -(learning rate) updates a weight
  * matrix in place. NaN or inf in G makes that matrix's update NaN.
- * out_dt also chooses the products' precision: DP_F32 comes within about 1e-6
- * (as a norm) of exact arithmetic, 2e-6 for small matrices; DP_BF16
- * rounds the operands of matrices of more than 64 rows and columns to 11 bits, of the order of the
- * result's own rounding for sums under noise (1e-3 to 1.5e-3 of the result; more
- * where a few directions outweigh all others: 7e-3 at 30 times their norm).
- * Between steps singular values s must stay below 8 and a + b s^2 + c s^4 below
- * 64 in magnitude, as they do for the usual coefficients (3.4445, -4.7750,
+ * out_dt also chooses the products' precision. Errors as norms, relative to the result, for the
+ * usual coefficients and ||G||_F of at least eps:
+ *  - DP_F32: that of the same steps in 32-bit products (at most twice it), 1e-6 to 2e-6 for sums
+ *    under noise. It grows where a few directions outweigh all others, as in a
+ *    momentum, since the others grow 485-fold in five steps: 5e-6 at 30 times their norm, 1.5e-5 at
+ *    100, 3e-5 for a matrix of rank 8.
+ *  - DP_BF16: the products' operands are rounded to 11 bits in matrices of more than 64 rows and
+ *    columns, while X itself is held in 22 before all but the last two steps: half a step of bf16 (2^-8 = 3.9e-3)
+ *    in all for any matrix, of which the result's own rounding is 1.7e-3 (sums under noise 1.8e-3 to
+ *    2.2e-3, rank 8 3.2e-3).
+ * Between steps singular values s must stay below 7.99, and a + b s^2 + c s^4 and b s^2 + c s^4 below
+ * 63.9 in magnitude, as they do for the usual coefficients (3.4445, -4.7750,
  * 2.0315; or 15/8, -10/8, 3/8); beyond, the update becomes inf or NaN.
  * Sides up to 65536 and, padded to multiples of 128, fewer than 2^30 elements (else
  * DP_EUNSUPPORTED), 1 <= steps <= 64. The workspace is dp_orthogonalize_workspace()
- * bytes, 16-byte aligned: about 8 bytes an element of G for DP_F32 and 4 for
- * DP_BF16, and 8 or 4 m^2 more for a shorter side m, for the 48 largest matrices; 0 where
+ * bytes, 16-byte aligned: about 8 bytes an element of G, and 8 m^2 (DP_F32) or 4 m^2 (DP_BF16)
+ * more for a shorter side m, for the 48 largest matrices; 0 where
  * all matrices are small enough to be worked in LDS (about 64 x 376 for DP_F32, 128 x 224 or
  * 64 x 512 for DP_BF16).
  * ------------------------------------------------------------------- */

@@ -543,7 +543,11 @@ struct NsArgs {
   int32_t n;
   int32_t out_dt, accumulate;
   int32_t step, last;
-  float coef[3];
+  float coef[3];          // of I, A and A^2 in P
+  // One plane (0 with two): X goes into the update by itself, times own, from both planes of its
+  // buffer (P then has no I); the next X's second plane is written too.
+  float own;
+  int32_t fine_next;
   float eps;
   uint32_t xcd_begin[9];  // items of XCD x: [xcd_begin[x], xcd_begin[x + 1])
   int32_t ks;             // ranges of k of a symmetric product's tile
@@ -565,12 +569,15 @@ DPG_HD inline int ns_parts(int rows, int cols) {
   const int64_t p = ((int64_t)rows * cols + 32767) / 32768;
   return p < 1 ? 1 : p > NS_PARTS ? NS_PARTS : (int)p;
 }
-// Offset of plane `plane` (of pl) of buffer `which`: X^T [np, mp] twice, A and P [mp, mp].
+// Offset of plane `plane` of buffer `which`: X^T [np, mp] twice, two planes each, A and P [mp, mp]
+// of pl planes.
 DPG_HD inline size_t ns_offset(int mp, int np, int which, int plane, int pl) {
   const size_t y = (size_t)mp * np * 2, q = (size_t)mp * mp * 2;
-  const size_t at = which <= NS_A ? (size_t)which * pl * y : 2 * (size_t)pl * y + (size_t)pl * q;
+  const size_t at = which <= NS_A ? (size_t)which * 2 * y : 4 * y + (size_t)pl * q;
   return NS_HEAD + at + (size_t)plane * (which < NS_A ? y : q);
 }
+// Whether X before step k of `steps` is held in two planes with one-plane products: not the last two.
+DPG_HD inline bool ns_fine(int k, int steps) { return k < steps - 2; }
 DPG_HD inline size_t ns_bytes(int mp, int np, int pl) {
   return ns_offset(mp, np, NS_P, 0, pl) + (size_t)pl * mp * mp * 2;
 }

@@ -6,21 +6,28 @@
 // and out = (prior) + scale X. A and A^2 are symmetric: only tiles on and above
 // the diagonal are computed, and stored twice. So a step costs
 // m(m+1)n + m^2(m+1) + 2 m^2 n operations in three launches for the whole group. Bound by the
-// matrix cores: GPT-2's 48 block matrices 98 us for A, 43 for A^2 and 163 for the update (800
-// TFLOP/s), 1.6 ms in five steps; 1601 x 6397 with two planes 104 us an update (950 TFLOP/s of fp16
-// products), 1.04 ms in five steps.
+// matrix cores, where launches have whole rounds of long tiles: GPT-2's 48 block matrices 98 us for A,
+// 43 for A^2 and 165 for the update (790 TFLOP/s), 205 to 245 where it carries X by itself (510 MB
+// more to move), 1.85 ms in five steps; 1601 x 6397 with two planes 104 us an update (950 TFLOP/s of
+// fp16 products), 1.0 ms in five steps.
 //
 // The products run on the fp16 matrix cores. Singular values are at most about
 // 1.2 on the way, so that X, held as 2^12 X, and A and P, held as 2^10 A and
 // 2^10 P, lie well inside fp16's range: its 11 bits round 8 times finer than
 // bf16's at the same rate.
-//   PL = 1 (bf16 results): one fp16 plane per operand. Five steps on noisy sums
-//     come to 1.1e-3 to 1.5e-3 of the result against fp64, and rounding the
-//     result to bf16 is 1.7e-3 by itself. (It grows with ||G||_F over the
-//     size of what lies beside G's leading directions: 3e-3 at 10, 7e-3 at 30.)
+//   PL = 1 (bf16 results): one fp16 plane per operand of a product. X itself is held in two,
+//     and the update takes a X from both, X <- a X + (b A + c A^2) x0: what is rounded off X falls on
+//     all its directions, and those beside a few leading ones grow a-fold a step (485-fold in
+//     five; with one plane, whose error is 1.4e-4 of X, a matrix of rank 8 came out 4.8e-2 off). The
+//     last two states make do with one plane and P = aI + ...: there b A + c A^2 is as large as a, and
+//     a X without the product of x1 would be further off than neither. Five steps on noisy
+//     sums come to 0.9e-3 to 1.4e-3 of the result against fp64, at rank 8 to 2.7e-3, and
+//     rounding the result to bf16 is 1.7e-3 by itself.
 //   PL = 2 (fp32 results): two planes, x = x0 + x1 with x1 what is left (22 bits
 //     together), and the three products x0 y0 + x0 y1 + x1 y0; x1 y1 is below
-//     2^-22. 0.6e-6 to 1.9e-6 in all (32-bit library products: 1.3e-6 to 4.4e-6).
+//     2^-22. 0.6e-6 to 1.9e-6 in all (32-bit library products: 1.3e-6 to 4.4e-6), growing as theirs
+//     do beside a few leading directions (512 x 1024 with rank 8 over noise of a thirtieth of its norm:
+//     4.4e-6, 32-bit products 3.6e-6; without noise 2.8e-5 and 2.3e-5).
 // Sums are fp32 in the matrix cores, the Frobenius norm is in fp64.
 //
 // Layout: m and n are padded with zeros to multiples of a tile, so that the
@@ -105,7 +112,7 @@ __device__ __forceinline__ void ns_cut(float (&v)[8], f16x8 (&h)[PL]) {
     }
 }
 
-// Y_0 from G: workgroup = 64 x 64 of the padded Y.
+// Y_0 from G: workgroup = 64 x 64 of the padded Y. Both planes, or (PL = 1, not a.fine_next) one.
 template <int DT, int PL, bool NT>
 __global__ __launch_bounds__(256) void ns_convert_kernel(NsArgs args) {
   const NsArgs& a = *(const NsArgs*)__builtin_amdgcn_kernarg_segment_ptr();
@@ -155,11 +162,12 @@ __global__ __launch_bounds__(256) void ns_convert_kernel(NsArgs args) {
     float x[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) x[e] = tile[r][k + e];
-    f16x8 h[PL];
-    ns_cut<PL>(x, h);
+    f16x8 h[2];
+    ns_cut<2>(x, h);
 #pragma unroll
-    for (int p = 0; p < PL; ++p)
-      *(f16x8*)((char*)ns_plane(M, NS_Y0, p, PL) + ns_at(i0 + r, (j0 + kb) / 32, q, M.mp)) = h[p];
+    for (int p = 0; p < 2; ++p)
+      if (p < PL || a.fine_next)
+        *(f16x8*)((char*)ns_plane(M, NS_Y0, p, PL) + ns_at(i0 + r, (j0 + kb) / 32, q, M.mp)) = h[p];
   }
 }
 
@@ -257,22 +265,31 @@ __device__ __forceinline__ void ns_poly(float (&v)[8], const float (&x)[8], cons
 }
 
 // A 32 x 32 block of the slice to rows row0 .. and columns col0 .. of a buffer: two KBs,
-// one per 16 rows. POLY adds its other terms from `have`, A's chunks of the same places.
-template <int PL>
+// one per 16 rows. POLY and (with one plane) UPDATE add other terms from `have`, the chunks of A or X
+// of the same places.
+template <int P>
 struct NsHave {
-  f16x8 y[2][PL];
-  __device__ __forceinline__ void load(const NsMat& M, int row0, int col0, int lane) {
+  f16x8 y[2][P];
+  __device__ __forceinline__ void load(const NsMat& M, int which, int pl, int row0, int col0, int lane) {
 #pragma unroll
     for (int it = 0; it < 2; ++it)
 #pragma unroll
-      for (int p = 0; p < PL; ++p)
-        y[it][p] = *(const f16x8*)((const char*)ns_plane(M, NS_A, p, PL) +
+      for (int p = 0; p < P; ++p)
+        y[it][p] = *(const f16x8*)((const char*)ns_plane(M, which, p, pl) +
                                    ns_at(row0 + (lane >> 2) + 16 * it, col0 / 32, lane & 3, M.mp));
   }
+  __device__ __forceinline__ void sum(int it, float (&x)[8]) const {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = (float)y[it][P - 1][e];
+#pragma unroll
+    for (int p = P - 2; p >= 0; --p)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] += (float)y[it][p][e];
+  }
 };
-template <int PL, int KIND>
+template <int PL, int KIND, int P>
 __device__ __forceinline__ void ns_keep(const NsArgs& a, const NsMat& M, const float* slice, int lane, int row0,
-                                        int col0, int dst, const NsHave<PL>& have) {
+                                        int col0, int dst, const NsHave<P>& have) {
 #pragma unroll
   for (int it = 0; it < 2; ++it) {
     const int r = (lane >> 2) + 16 * it, q = lane & 3, c = ns_chunk(r, q) * 8;
@@ -280,20 +297,27 @@ __device__ __forceinline__ void ns_keep(const NsArgs& a, const NsMat& M, const f
     ns_take(slice, r, c, v);
     const int64_t at = ns_at(row0 + r, col0 / 32, q, M.mp);
     if constexpr (KIND == NS_POLY) {
-      float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int p = PL - 1; p >= 0; --p)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] += (float)have.y[it][p][e];
+      float x[8];
+      have.sum(it, x);
       ns_poly(v, x, a.coef, row0 + r, col0 + c);
     } else {
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[e] *= KIND == NS_GRAM ? NS_SA / (NS_SX * NS_SX) : 1.f / NS_SA;
     }
-    f16x8 h[PL];
-    ns_cut<PL>(v, h);
+    constexpr bool FINE = KIND == NS_UPDATE && PL == 1;
+    if constexpr (FINE)
+      if (a.own != 0.f) {
+        float x[8];
+        have.sum(it, x);
 #pragma unroll
-    for (int p = 0; p < PL; ++p) {
+        for (int e = 0; e < 8; ++e) v[e] = fmaf(a.own, x[e], v[e]);
+      }
+    constexpr int TO = FINE ? 2 : PL;
+    f16x8 h[TO];
+    ns_cut<TO>(v, h);
+#pragma unroll
+    for (int p = 0; p < TO; ++p) {
+      if (p >= PL && !a.fine_next) continue;
       f16x8* to = (f16x8*)((char*)ns_plane(M, dst, p, PL) + at);
       // Y is read by other XCDs next, and is larger than the L2s.
       if constexpr (KIND == NS_UPDATE) __builtin_nontemporal_store(h[p], to); else *to = h[p];
@@ -544,16 +568,28 @@ __global__ __launch_bounds__(256, (NsShape<PL, FM, FN>::GROUPS)) void ns_gemm_ke
 #pragma unroll
       for (int j = 0; j < FN; ++j) {
         const int bi = i0 + wm + i * 32, bj = j0 + wn + j * 32;
-        have[i][j][0].load(M, bj, bi, lane);
-        have[i][j][1].load(M, bi, bj, lane);
+        have[i][j][0].load(M, NS_A, PL, bj, bi, lane);
+        have[i][j][1].load(M, NS_A, PL, bi, bj, lane);
       }
+  }
+  // X by itself (see a.own), DEEP blocks ahead of where it is added.
+  constexpr bool FINE = KIND == NS_UPDATE && PL == 1;
+  constexpr int DEEP = FINE ? (FM * FN < 4 ? FM * FN : 4) : 1;
+  NsHave<2> mine[DEEP];
+  const int jn = SYM ? M.mp : M.np;
+  auto want = [&](int blk) __attribute__((always_inline)) {
+    const int bi = i0 + wm + blk / FN * 32, bj = j0 + wn + blk % FN * 32;
+    if (a.own != 0.f && bi < M.mp && bj < jn) mine[blk % DEEP].load(M, y_now, PL, bj, bi, lane);
+  };
+  if constexpr (FINE) {
+#pragma unroll
+    for (int blk = 0; blk < DEEP; ++blk) want(blk);
   }
   ns_wait<0>();   // loads past the end still write the ring
   __syncthreads();
 
   // Epilogue, one 32 x 32 block at a time through the wave's own slice.
   float* slice = (float*)ring + w * 32 * NS_EP_LD;
-  const int jn = SYM ? M.mp : M.np;
 #pragma unroll
   for (int i = 0; i < FM; ++i) {
 #pragma unroll
@@ -570,12 +606,17 @@ __global__ __launch_bounds__(256, (NsShape<PL, FM, FN>::GROUPS)) void ns_gemm_ke
         const int hi = POLY ? i : 0, hj = POLY ? j : 0;
         if (in) {
           ns_fill<false>(slice, acc[i][j], lane);
-          ns_keep<PL, KIND>(a, M, slice, lane, bj, bi, SYM ? dst : y_next, have[hi][hj][0]);
+          if constexpr (FINE)
+            ns_keep<PL, KIND>(a, M, slice, lane, bj, bi, y_next, mine[(i * FN + j) % DEEP]);
+          else
+            ns_keep<PL, KIND>(a, M, slice, lane, bj, bi, SYM ? dst : y_next, have[hi][hj][0]);
           if (SYM && ti != tj) {
             ns_fill<true>(slice, acc[i][j], lane);
             ns_keep<PL, KIND>(a, M, slice, lane, bi, bj, dst, have[hi][hj][1]);
           }
         }
+        if constexpr (FINE)
+          if (i * FN + j + DEEP < FM * FN) want(i * FN + j + DEEP);
       }
     }
   }
@@ -599,8 +640,8 @@ __global__ __launch_bounds__(256) void ns_join_kernel(NsArgs args) {
   const int bj = tj * NS_TILE + (int)(quarter & 1) * 64 + (w & 1) * 32;
   NsHave<PL> have[2];
   if constexpr (KIND == NS_POLY) {
-    have[0].load(M, bj, bi, lane);
-    have[1].load(M, bi, bj, lane);
+    have[0].load(M, NS_A, PL, bj, bi, lane);
+    have[1].load(M, NS_A, PL, bi, bj, lane);
   }
   f32x16 c = {};
 #pragma unroll 4
@@ -622,7 +663,8 @@ __global__ __launch_bounds__(256) void ns_join_kernel(NsArgs args) {
 
 // All steps of a matrix in one workgroup, its Y, A and P in LDS as the buffers' blocks (see
 // above; sides padded to 32, blocks along mp). A wave takes every eighth 32 x 32 block
-// of a product. An update's blocks stay in registers until every wave has read Y.
+// of a product. An update's blocks stay in registers until every wave has read Y. With one plane X's
+// blocks also stay there, in fp32, for as long as X goes into the update by itself (ns_fine).
 // Bound by latency: fifteen products in a row, each a barrier, a chain of LDS reads and the turn
 // through the slice. (Four matrices of a block of width 64, five steps, fp32 results: 41 us; in 17
 // launches of 5 to 9 us each 143.)
@@ -745,9 +787,32 @@ __global__ __launch_bounds__(NS_SMALL_WAVES * WAVE) void ns_small_kernel(NsArgs 
     };
   };
 
+  // X, as Y is held (times NS_SX), where the matrix instructions leave its blocks.
+  f32x16 X[PL == 1 ? NS_SMALL_BLOCKS : 1];
+  if (PL == 1 && ns_fine(0, a.steps)) {
+#pragma unroll
+    for (int u = 0; u < NS_SMALL_BLOCKS; ++u) {
+      const int t = w + u * W;
+      if (t < mb * nb)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const int i = 32 * (t % mb) + 8 * (e >> 2) + 4 * (lane >> 5) + (e & 3), j = 32 * (t / mb) + fr;
+          const int r = flip ? i : j, c = flip ? j : i;
+          float g = 0.f;
+          if (r < M.rows && c < M.cols) {
+            const int64_t at = (int64_t)r * M.ldg + c;
+            g = DT == DT_BF16 ? bf16_to_f32(((const uint16_t*)M.G)[at]) : ((const float*)M.G)[at];
+            g = (float)((double)g * f);
+          }
+          X[PL == 1 ? u : 0][e] = g;
+        }
+    }
+  }
+
   for (int step = 0; step < a.steps; ++step) {
     const float* coef = coefs.c + 3 * step;
-    const float cf[3] = {coef[0], coef[1], coef[2]};
+    const bool fine = PL == 1 && ns_fine(step, a.steps);
+    const float cf[3] = {fine ? 0.f : coef[0], coef[1], coef[2]};
     auto poly = [&](float (&v)[8], int at, int row, int col) __attribute__((always_inline)) {
       float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -784,6 +849,10 @@ __global__ __launch_bounds__(NS_SMALL_WAVES * WAVE) void ns_small_kernel(NsArgs 
       if (t < mb * nb)
         c[u] = product(mp / 16, [&](int p, int k) { return rows(P + p * planeA, t % mb, k); },
                        [&](int p, int k) { return rows(Y + p * planeY, t / mb, k); });
+      if (fine) {
+        c[u] += coef[0] * NS_SA * X[PL == 1 ? u : 0];
+        X[PL == 1 ? u : 0] = c[u] * (1.f / NS_SA);
+      }
     }
     const bool last = step == a.steps - 1;
     __syncthreads();
@@ -877,8 +946,8 @@ static hipError_t ns_symmetric(NsArgs& a, const NsBins& bins, hipStream_t s) {
 // Large tiles: 128 x 128 for the symmetric products, whose launches have few; for updates
 // 128 x 256 with one plane (fewer LDS reads per product: 171 us for GPT-2's blocks, 197 with 128 x
 // 128), the last 190 us (200 with 256 x 256, which waits for its stores), 128 x 128 with two (105 us
-// for 1601 x 6397, 116 with 256 x 128, which leave no room for a second workgroup and more of the last
-// round empty; 367 and 331 for 4096 x 4096).
+// for 1601 x 6397, three rounds, and 331 for 4096 x 4096; with 256 x 128, whose ring has three stages
+// instead of four, 116, two rounds of twice the length, and 367; either way a CU holds one workgroup).
 template <int PL>
 static hipError_t ns_step(NsArgs& a, const NsBins& bins, hipStream_t s) {
   constexpr int FN = PL == 1 ? 4 : 2;
@@ -889,8 +958,11 @@ static hipError_t ns_step(NsArgs& a, const NsBins& bins, hipStream_t s) {
   if (a.last)
     return plan.small ? ns_launch<PL, NS_LAST, 1, 1, false>(a, bins, s) : ns_launch<PL, NS_LAST, 2, FN, false>(a, bins, s);
   if (plan.small) return ns_launch<PL, NS_UPDATE, 1, 1, false>(a, bins, s);
+  // With X by itself a tile's end moves three times as much, beside which a second workgroup works
+  // (128 x 256 and 256 x 256, all five steps, us: GPT-2's blocks 1845, 1917; 24 x (1024 x 1024, 1024 x
+  // 4096) 1745, 1808; 4096 x 4096 1668, 1664; 4096 x 16384 5063, 5038).
   if constexpr (PL == 1)
-    if (plan.wide) return ns_launch<PL, NS_UPDATE, 4, 4, false>(a, bins, s);
+    if (plan.wide && a.own == 0.f) return ns_launch<PL, NS_UPDATE, 4, 4, false>(a, bins, s);
   return ns_launch<PL, NS_UPDATE, 2, FN, false>(a, bins, s);
 }
 
@@ -918,9 +990,16 @@ static hipError_t ns_run(NsArgs a, const float* coef, int steps, hipStream_t s) 
   const NsBins bins = ns_order(a);
   int64_t bytes = 0;
   for (int l = 0; l < a.n; ++l) bytes += (int64_t)a.M[l].rows * a.M[l].cols * Oct<DT>::ES;
+  a.fine_next = PL == 1 && ns_fine(0, steps) ? 1 : 0;
   hipError_t e = bytes > ((int64_t)256 << 20) ? ns_begin<DT, PL, true>(a, s) : ns_begin<DT, PL, false>(a, s);
   for (int k = 0; k < steps && e == hipSuccess; ++k) {
     for (int q = 0; q < 3; ++q) a.coef[q] = coef[3 * k + q];
+    a.own = 0.f;
+    if (PL == 1 && ns_fine(k, steps)) {
+      a.own = a.coef[0];
+      a.coef[0] = 0.f;
+    }
+    a.fine_next = PL == 1 && ns_fine(k + 1, steps) ? 1 : 0;
     a.step = k;
     a.last = k == steps - 1 ? 1 : 0;
     e = ns_step<PL>(a, bins, s);
