@@ -479,7 +479,7 @@ inline LnPlan ln_plan(int B, int T, int d, bool grads) {
   p.span = (int32_t)((T + ranges - 1) / ranges);
   p.ranges = (int32_t)(((int64_t)T + p.span - 1) / p.span);
   // One workgroup per example adds few ranges (a chain of loads each); more are added by
-  // chunks of 64 features, and an example's norm by a third launch.
+  // chunks of 64 features, and the norms of more than one chunk by a third launch.
   p.chunks = p.ranges <= LN_FEW ? 1 : (d + 63) / 64;
   return p;
 }
