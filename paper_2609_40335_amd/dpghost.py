@@ -183,14 +183,23 @@ def _dtype(t: torch.Tensor) -> int:
     raise DPError(f"unsupported dtype {t.dtype}")
 
 
+def _row_stride(shape, st):
+    """The distance of a [B, T, w] view's token rows, None if it has no single one. With one
+    token an example that is the examples' distance (z[:, -1:, :], say)."""
+    B, T, w = shape
+    if st[2] != 1 or (B > 1 and T > 1 and st[0] != T * st[1]):
+        return None
+    return st[1] if T > 1 else st[0] if B > 1 else max(st[1], w)
+
+
 def _rows(t: torch.Tensor, name: str):
     """(pointer, B, T, width, row stride) of a token-major [B, T, w] tensor."""
     if t.dim() != 3:
         raise DPError(f"{name} must be [B, T, w]")
-    B, T, w = t.shape
-    if t.stride(2) != 1 or (B > 1 and t.stride(0) != T * t.stride(1)):
+    ld = _row_stride(t.shape, t.stride())
+    if ld is None:
         raise DPError(f"{name} must have unit feature stride and uniformly spaced token rows")
-    return t.data_ptr(), B, T, w, t.stride(1)
+    return (t.data_ptr(), *t.shape, ld)
 
 
 def _dev(t: torch.Tensor, name: str) -> None:
@@ -776,9 +785,9 @@ def _f32(t, shape, name: str):
 def _tokens(t, name: str):
     """(pointer, [B, T, w], row stride) of a token-major tensor, as _rows checks it."""
     shape, st = t.shape, t.stride()
-    if len(shape) != 3 or st[2] != 1 or (shape[0] > 1 and st[0] != shape[1] * st[1]):
-        _rows(t, name)
-    return t.data_ptr(), shape, st[1]
+    if len(shape) == 3 and st[2] == 1 and st[0] == shape[1] * st[1] and st[1] >= shape[2]:
+        return t.data_ptr(), shape, st[1]   # the common case, as cheap as it can be
+    return t.data_ptr(), shape, _rows(t, name)[4]
 
 
 def _like(t, shape, dtype, name: str, of: str):
@@ -854,7 +863,9 @@ def _logits(Z, targets):
 
 def dp_token_logprobs(Z, targets, logp, lse=None, stream=None) -> torch.Tensor:
     """logp [B, T] = log softmax(Z)[target] (0 where the target is outside [0, V)),
-    lse [B, T] the logarithm of the row's sum of exponentials."""
+    lse [B, T] the logarithm of the row's sum of exponentials. Rows are evenly spaced: the last
+    token of every prompt is Z[:, -1:, :]; for all but the last pass Z whole, with a last
+    target of -1."""
     raw = _same_device(stream, (Z, "Z"), (targets, "targets"), (logp, "logp"), (lse, "lse"))
     pz, shape, ldz = _logits(Z, targets)
     B, T, V = shape
