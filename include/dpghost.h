@@ -616,10 +616,11 @@ dp_status_t dp_preference_loss(const void* Z, int64_t ldz, const int32_t* target
  * 2.0315; or 15/8, -10/8, 3/8); beyond, the update becomes inf or NaN.
  * Sides up to 65536 and, padded to multiples of 128, fewer than 2^30 elements (else
  * DP_EUNSUPPORTED), 1 <= steps <= 64. The workspace is dp_orthogonalize_workspace()
- * bytes, 16-byte aligned: about 8 bytes an element of G, and 8 m^2 (DP_F32) or 4 m^2 (DP_BF16)
- * more for a shorter side m, for the 48 largest matrices; 0 where
- * all matrices are small enough to be worked in LDS (about 64 x 376 for DP_F32, 128 x 224 or
- * 64 x 512 for DP_BF16).
+ * bytes, 16-byte aligned. For the 48 matrices of a group that need most: with sides padded to
+ * multiples of 128, m the shorter and n the longer one, 8 m n bytes and 8 m^2 more, or 4 m^2 for
+ * DP_BF16 where both sides exceed 64, and about 1 KB; and, where large matrices are
+ * few, up to 128 MiB for sums in parts. 0 where all are small enough to be worked in LDS (32 x 896 and
+ * 64 x 352 for both, 96 x 128 for DP_F32, 96 x 320 and 128 x 224 for DP_BF16, or the transpose).
  * ------------------------------------------------------------------- */
 typedef struct {
   const void* G;
