@@ -608,9 +608,10 @@ dp_status_t dp_preference_loss(const void* Z, int64_t ldz, const int32_t* target
  *    momentum, since the others grow 485-fold in five steps: 5e-6 at 30 times their norm, 1.5e-5 at
  *    100, 3e-5 for a matrix of rank 8.
  *  - DP_BF16: the products' operands are rounded to 11 bits in matrices of more than 64 rows and
- *    columns, while X itself is held in 22 before all but the last two steps: half a step of bf16 (2^-8 = 3.9e-3)
- *    in all for any matrix, of which the result's own rounding is 1.7e-3 (sums under noise 1.8e-3 to
- *    2.2e-3, rank 8 3.2e-3).
+ *    columns, while X itself is held in 22 before all but the last two steps: within half a step
+ *    of bf16, 2^-8 = 3.9e-3, in all (sums under noise 1.8e-3 to 2.2e-3, momenta up to 3.4e-3, at rank
+ *    1), of which the result's own rounding is 1.7e-3. Matrices of a few distinct values,
+ *    whose roundings agree, come to 5e-3.
  * Between steps singular values s must stay below 7.99, and a + b s^2 + c s^4 and b s^2 + c s^4 below
  * 63.9 in magnitude, as they do for the usual coefficients (3.4445, -4.7750,
  * 2.0315; or 15/8, -10/8, 3/8); beyond, the update becomes inf or NaN.

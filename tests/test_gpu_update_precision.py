@@ -74,6 +74,21 @@ def test_signal_over_noise(dp, m, n, signal):
         assert err <= bound, (m, n, signal, dt)
 
 
+@pytest.mark.parametrize("rank", [1, 2, 32])
+@pytest.mark.parametrize("m,n", [(512, 1024), (96, 200), (700, 130)])
+def test_low_ranks_without_noise(dp, m, n, rank):
+    g = np.random.default_rng(rank)
+    G = (g.standard_normal((m, rank)) @ g.standard_normal((rank, n))).astype(np.float32)
+    ref = F.newton_schulz(G.astype(np.float64), MUON, float(np.float32(1e-7)))
+    size, plain = np.linalg.norm(ref), np.linalg.norm(_in_32_bits(G) - ref)
+    for dt, bound in ((torch.float32, 2 * plain + 2.0 ** -24 * size), (torch.bfloat16, 2.0 ** -8 * size)):
+        out = torch.empty(m, n, dtype=dt, device="cuda")
+        dp.dp_orthogonalize_grouped([torch.from_numpy(G).cuda()], [out])
+        err = np.linalg.norm(out.cpu().double().numpy() - ref)
+        print(f"  {m}x{n} rank {rank} {dt}: {err / size:.2e}, allowed {bound / size:.2e}", flush=True)
+        assert err <= bound, (m, n, rank, dt)
+
+
 @pytest.mark.parametrize("out", [torch.float32, torch.bfloat16])
 def test_every_matrix_of_a_large_group(dp, out):
     """48 and more matrices of GPT-2's shapes and ragged ones, each against 64 bits (on the GPU)."""
