@@ -544,10 +544,8 @@ struct NsArgs {
   int32_t out_dt, accumulate;
   int32_t step, last;
   float coef[3];          // of I, A and A^2 in P
-  // One plane (0 with two): X goes into the update by itself, times own, from both planes of its
-  // buffer (P then has no I); the next X's second plane is written too.
-  float own;
-  int32_t fine_next;
+  float own;              // X goes into the update by itself, times this (P then has no I)
+  int32_t fine_next;      // one plane: the next X's second plane is written too
   float eps;
   uint32_t xcd_begin[9];  // items of XCD x: [xcd_begin[x], xcd_begin[x + 1])
   int32_t ks;             // ranges of k of a symmetric product's tile
@@ -576,8 +574,8 @@ DPG_HD inline size_t ns_offset(int mp, int np, int which, int plane, int pl) {
   const size_t at = which <= NS_A ? (size_t)which * 2 * y : 4 * y + (size_t)pl * q;
   return NS_HEAD + at + (size_t)plane * (which < NS_A ? y : q);
 }
-// Whether X before step k of `steps` is held in two planes with one-plane products: not the last two.
-DPG_HD inline bool ns_fine(int k, int steps) { return k < steps - 2; }
+// Whether X goes into step k's update by itself, from two planes whatever the products have.
+DPG_HD inline bool ns_fine(int k, int steps, int pl) { return k < steps - (pl == 1 ? 2 : 1); }
 DPG_HD inline size_t ns_bytes(int mp, int np, int pl) {
   return ns_offset(mp, np, NS_P, 0, pl) + (size_t)pl * mp * mp * 2;
 }

@@ -15,19 +15,21 @@
 // 1.2 on the way, so that X, held as 2^12 X, and A and P, held as 2^10 A and
 // 2^10 P, lie well inside fp16's range: its 11 bits round 8 times finer than
 // bf16's at the same rate.
-//   PL = 1 (bf16 results): one fp16 plane per operand of a product. X itself is held in two,
-//     and the update takes a X from both, X <- a X + (b A + c A^2) x0: what is rounded off X falls on
-//     all its directions, and those beside a few leading ones grow a-fold a step (485-fold in
-//     five; with one plane, whose error is 1.4e-4 of X, a matrix of rank 8 came out 4.8e-2 off). The
-//     last two states make do with one plane and P = aI + ...: there b A + c A^2 is as large as a, and
+// What is rounded off X, or off a in P = aI + b A + c A^2, falls on all directions of X, and those
+// beside a few leading ones grow a-fold a step (485-fold in five). So X is held in two planes, and
+// goes into the update by itself, X <- a X + (b A + c A^2) X, in 32 bits (see a.own).
+//   PL = 1 (bf16 results): one fp16 plane per operand of a product, whose error is 2e-4 of
+//     X (with nothing else, a matrix of rank 8 came out 4.8e-2 off). The last two states of X
+//     make do with it, and with P = aI + ...: there b A + c A^2 is as large as a, and
 //     a X without the product of x1 would be further off than neither. Five steps on noisy
 //     sums come to 0.9e-3 to 1.4e-3 of the result against fp64, at rank 8 to 2.7e-3, and
 //     rounding the result to bf16 is 1.7e-3 by itself.
 //   PL = 2 (fp32 results): two planes, x = x0 + x1 with x1 what is left (22 bits
 //     together), and the three products x0 y0 + x0 y1 + x1 y0; x1 y1 is below
-//     2^-22. 0.6e-6 to 1.9e-6 in all (32-bit library products: 1.3e-6 to 4.4e-6), growing as theirs
-//     do beside a few leading directions (512 x 1024 with rank 8 over noise of a thirtieth of its norm:
-//     4.4e-6, 32-bit products 3.6e-6; without noise 2.8e-5 and 2.3e-5).
+//     2^-22. Never further off than 32-bit products: 1e-6 for sums under noise (theirs 1.3e-6 to
+//     4.4e-6), growing as theirs do beside a few leading directions (512 x 1024 of rank 8 1.7e-5, theirs
+//     2.0e-5; of rank 32 1.0e-5 and 1.1e-5, with P = aI + ... in every step 2.0e-5). The last step,
+//     whose roundings grow no more, has its a in P.
 // Sums are fp32 in the matrix cores, the Frobenius norm is in fp64.
 //
 // Layout: m and n are padded with zeros to multiples of a tile, so that the
@@ -265,8 +267,7 @@ __device__ __forceinline__ void ns_poly(float (&v)[8], const float (&x)[8], cons
 }
 
 // A 32 x 32 block of the slice to rows row0 .. and columns col0 .. of a buffer: two KBs,
-// one per 16 rows. POLY and (with one plane) UPDATE add other terms from `have`, the chunks of A or X
-// of the same places.
+// one per 16 rows. POLY and UPDATE add other terms from `have`, the chunks of A or X of the same places.
 template <int P>
 struct NsHave {
   f16x8 y[2][P];
@@ -304,7 +305,7 @@ __device__ __forceinline__ void ns_keep(const NsArgs& a, const NsMat& M, const f
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[e] *= KIND == NS_GRAM ? NS_SA / (NS_SX * NS_SX) : 1.f / NS_SA;
     }
-    constexpr bool FINE = KIND == NS_UPDATE && PL == 1;
+    constexpr bool FINE = KIND == NS_UPDATE;
     if constexpr (FINE)
       if (a.own != 0.f) {
         float x[8];
@@ -312,7 +313,7 @@ __device__ __forceinline__ void ns_keep(const NsArgs& a, const NsMat& M, const f
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] = fmaf(a.own, x[e], v[e]);
       }
-    constexpr int TO = FINE ? 2 : PL;
+    constexpr int TO = KIND == NS_UPDATE ? 2 : PL;
     f16x8 h[TO];
     ns_cut<TO>(v, h);
 #pragma unroll
@@ -573,7 +574,7 @@ __global__ __launch_bounds__(256, (NsShape<PL, FM, FN>::GROUPS)) void ns_gemm_ke
       }
   }
   // X by itself (see a.own), DEEP blocks ahead of where it is added.
-  constexpr bool FINE = KIND == NS_UPDATE && PL == 1;
+  constexpr bool FINE = KIND == NS_UPDATE;
   constexpr int DEEP = FINE ? (FM * FN < 4 ? FM * FN : 4) : 1;
   NsHave<2> mine[DEEP];
   const int jn = SYM ? M.mp : M.np;
@@ -789,7 +790,7 @@ __global__ __launch_bounds__(NS_SMALL_WAVES * WAVE) void ns_small_kernel(NsArgs 
 
   // X, as Y is held (times NS_SX), where the matrix instructions leave its blocks.
   f32x16 X[PL == 1 ? NS_SMALL_BLOCKS : 1];
-  if (PL == 1 && ns_fine(0, a.steps)) {
+  if (PL == 1 && ns_fine(0, a.steps, PL)) {
 #pragma unroll
     for (int u = 0; u < NS_SMALL_BLOCKS; ++u) {
       const int t = w + u * W;
@@ -811,7 +812,7 @@ __global__ __launch_bounds__(NS_SMALL_WAVES * WAVE) void ns_small_kernel(NsArgs 
 
   for (int step = 0; step < a.steps; ++step) {
     const float* coef = coefs.c + 3 * step;
-    const bool fine = PL == 1 && ns_fine(step, a.steps);
+    const bool fine = ns_fine(step, a.steps, PL);
     const float cf[3] = {fine ? 0.f : coef[0], coef[1], coef[2]};
     auto poly = [&](float (&v)[8], int at, int row, int col) __attribute__((always_inline)) {
       float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
@@ -849,7 +850,7 @@ __global__ __launch_bounds__(NS_SMALL_WAVES * WAVE) void ns_small_kernel(NsArgs 
       if (t < mb * nb)
         c[u] = product(mp / 16, [&](int p, int k) { return rows(P + p * planeA, t % mb, k); },
                        [&](int p, int k) { return rows(Y + p * planeY, t / mb, k); });
-      if (fine) {
+      if (PL == 1 && fine) {
         c[u] += coef[0] * NS_SA * X[PL == 1 ? u : 0];
         X[PL == 1 ? u : 0] = c[u] * (1.f / NS_SA);
       }
@@ -862,7 +863,15 @@ __global__ __launch_bounds__(NS_SMALL_WAVES * WAVE) void ns_small_kernel(NsArgs 
       if (t < mb * nb) {
         ns_fill<false>(slice, c[u], lane);
         if (last) ns_give(a, M, slice, lane, 32 * (t % mb), 32 * (t / mb));
-        else keep(Y, planeY, 32 * (t / mb), 32 * (t % mb), times(1.f / NS_SA));
+        else keep(Y, planeY, 32 * (t / mb), 32 * (t % mb), [&](float (&v)[8], int at, int, int) __attribute__((always_inline)) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) v[e] *= 1.f / NS_SA;
+          if constexpr (PL == 2) {   // the X that this one takes the place of
+            const f16x8 y0 = *(const f16x8*)(Y + at), y1 = *(const f16x8*)(Y + planeY + at);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = fmaf(coef[0], (float)y1[e] + (float)y0[e], v[e]);
+          }
+        });
       }
     }
   }
@@ -990,16 +999,16 @@ static hipError_t ns_run(NsArgs a, const float* coef, int steps, hipStream_t s) 
   const NsBins bins = ns_order(a);
   int64_t bytes = 0;
   for (int l = 0; l < a.n; ++l) bytes += (int64_t)a.M[l].rows * a.M[l].cols * Oct<DT>::ES;
-  a.fine_next = PL == 1 && ns_fine(0, steps) ? 1 : 0;
+  a.fine_next = ns_fine(0, steps, PL) ? 1 : 0;
   hipError_t e = bytes > ((int64_t)256 << 20) ? ns_begin<DT, PL, true>(a, s) : ns_begin<DT, PL, false>(a, s);
   for (int k = 0; k < steps && e == hipSuccess; ++k) {
     for (int q = 0; q < 3; ++q) a.coef[q] = coef[3 * k + q];
     a.own = 0.f;
-    if (PL == 1 && ns_fine(k, steps)) {
+    if (ns_fine(k, steps, PL)) {
       a.own = a.coef[0];
       a.coef[0] = 0.f;
     }
-    a.fine_next = PL == 1 && ns_fine(k + 1, steps) ? 1 : 0;
+    a.fine_next = ns_fine(k + 1, steps, PL) ? 1 : 0;
     a.step = k;
     a.last = k == steps - 1 ? 1 : 0;
     e = ns_step<PL>(a, bins, s);

@@ -89,6 +89,27 @@ def test_low_ranks_without_noise(dp, m, n, rank):
         assert err <= bound, (m, n, rank, dt)
 
 
+@pytest.mark.parametrize("noise", [0.0, 0.1])
+@pytest.mark.parametrize("m,n,rank", [(512, 1024, 32), (700, 1500, 128), (96, 200, 8), (60, 80, 32),
+                                      (768, 768, 512), (130, 60, 3)])
+def test_fp32_results_match_32_bit_products(dp, m, n, rank, noise):
+    """Beside the leading directions 32-bit products round three times a step (a X, the product
+    and their sum, each 2^-24 at most), the kernels once to 22 bits: with x = x0 + x1, x1's
+    half step is 2^-23 or, for a smaller x1, less, 0.76 of it as a root mean square. 0.76 x 2 / 3 ** 0.5 =
+    0.87 of their error; 1.25 leaves room for another sample."""
+    g = np.random.default_rng(rank)
+    G = g.standard_normal((m, rank)) @ g.standard_normal((rank, n))
+    N = g.standard_normal((m, n))
+    G = (G / np.linalg.norm(G) + noise * N / np.linalg.norm(N)).astype(np.float32)
+    ref = F.newton_schulz(G.astype(np.float64), MUON, float(np.float32(1e-7)))
+    plain = np.linalg.norm(_in_32_bits(G) - ref)
+    out = torch.empty(m, n, device="cuda")
+    dp.dp_orthogonalize_grouped([torch.from_numpy(G).cuda()], [out])
+    err = np.linalg.norm(out.cpu().double().numpy() - ref)
+    print(f"  {m}x{n} rank {rank} noise {noise}: {err / plain:.2f} of 32-bit products' error", flush=True)
+    assert err <= 1.25 * plain
+
+
 @pytest.mark.parametrize("out", [torch.float32, torch.bfloat16])
 def test_every_matrix_of_a_large_group(dp, out):
     """48 and more matrices of GPT-2's shapes and ragged ones, each against 64 bits (on the GPU)."""
