@@ -606,7 +606,7 @@ dp_status_t dp_preference_loss(const void* Z, int64_t ldz, const int32_t* target
  *  - DP_F32: that of the same steps in 32-bit products, about 1e-6 for sums
  *    under noise. It grows where a few directions outweigh all others, as in a
  *    momentum, since the others grow 485-fold in five steps: 3e-6 at 30 times their norm, 1e-5 at
- *    100, 2e-5 for a matrix of rank 8, 6e-5 at rank 1.
+ *    100, 2e-5 for a matrix of rank 8, 8e-5 at rank 1.
  *  - DP_BF16: the products' operands are rounded to 11 bits in matrices of more than 64 rows and
  *    columns, while X itself is held in 22 before all but the last two steps: within half a step
  *    of bf16, 2^-8 = 3.9e-3, in all (sums under noise 1.8e-3 to 2.2e-3, momenta up to 3.4e-3, at rank

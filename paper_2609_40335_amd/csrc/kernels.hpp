@@ -463,8 +463,9 @@ struct LnBackwardArgs {
 hipError_t launch_ln_backward(const LnBackwardArgs& a, int dt, hipStream_t s);
 
 // How the backward pass cuts an example's T rows: about LN_GROUPS workgroups in
-// all, but no fewer rows each than keep the partial sums' way to memory and back
-// (16 d bytes a range) below a quarter of the operands' (3 T d elements).
+// all, but about `least` rows each at least, beside whose operands (3 d elements a row) the partial
+// sums' way to memory and back (16 d bytes a range) stays small: a sixth in bf16 up to 2048 features, a third above,
+// half of that in fp32; up to twice that where T is little more than `least`, as T / least is rounded up.
 constexpr int LN_GROUPS = 512, LN_FEW = 32;
 struct LnPlan {
   int32_t ranges, span, chunks;
@@ -594,7 +595,8 @@ DPG_HD inline size_t ns_bytes(int mp, int np, int pl) {
 // and 100 x 3000 fp32, X X^T alone small: 144, 210; 1536 x 1536 fp32, updates alone: 419, 451.
 // Updates and X X^T with one plane that fill a round with 256 x 256 tiles take those: fewer LDS reads and
 // loads per product (us, such tiles and the others: updates 4096 x 4096 120, 131; 24 x (1024 x 1024, 1024 x
-// 4096) 281, 312; their X X^T 167, 184). A^2, whose other operand needs registers too, does not: 115, 95.
+// 4096) 281, 312; their X X^T 167, 184). A^2, whose other operand needs registers too, does not: 115, 95;
+// nor do updates that X goes into by itself (see ns_step).
 struct NsPlan {
   int ks;
   bool small, wide;       // 64 x 64 tiles; 256 x 256 tiles

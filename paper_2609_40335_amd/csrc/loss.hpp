@@ -11,8 +11,8 @@
 // so every scored token of the chosen answer has the weight
 // beta ((1 - eps) sigma(-m) - eps sigma(m)), and of the rejected one its negative.
 //
-// All of it is bound by HBM: a logit costs one exponential (three in the
-// passes that write gradients twice over) and moves 2 to 8 bytes. Cross-entropy
+// All of it is bound by HBM: a logit costs one exponential for its row's sum and
+// one for its gradient, and moves 2 to 12 bytes. Cross-entropy
 // keeps its row in registers between the sum and the gradient, so the logits
 // are read once (a row of 50257 is 98 KB in bf16: 7 units of 16 bytes a thread of
 // 1024). A pair's weight needs the last row's log p before the first row's
@@ -21,7 +21,7 @@
 // one pass, 688 two at a time, 832 one by one, for the launches' ends; nor were streaming loads in the
 // first pass, 684, or the rows backwards in the second, 670.)
 // Measured, rows of 50257 of which a third is not scored (and not read): bf16 log-probabilities of 24 x
-// 128 45 us (4.5 TB/s: few rows a CU, and an exponential for every 2 bytes), cross-entropy of 32 x 128
+// 128 42 us (4.8 TB/s: few rows a CU, and an exponential for every 2 bytes), cross-entropy of 32 x 128
 // 123 us (5.6 TB/s; a copy runs at 4.9), in fp32 of 24 x 100 158 us (5.1); a preference loss of 16 x 1024
 // tokens 657 us, 3.9 GB in two passes (5.9).
 //
@@ -41,7 +41,7 @@ constexpr float LOWEST = -FLT_MAX;   // running maximum of no logits (finite: -i
 template <int DT>
 constexpr uint32_t NEG_INF = DT == DT_BF16 ? 0xFF80FF80u : 0xFF800000u;
 
-// exp(d) for d <= 0. log2 e as one fp32 number is LOG2E_LOST off (1.3e-8 of itself), so that
+// exp(d) for d <= 0. log2 e as one fp32 number is LOST off (1.3e-8 of itself), so that
 // every exp(d) is off by d LOST of itself, the same way in every row: 6e-8 of a sum of
 // exponentials, which a sum of hundreds of log-probabilities shows. Such sums (EXACT) add
 // up d exp(d) as well and put the first order back. (As a second term of the exponent it would be
@@ -514,7 +514,7 @@ hipError_t launch_cross_entropy(const LossArgs& a, int dt, hipStream_t s) {
 template <int DT, bool NT>
 static hipError_t lg(LossArgs a, hipStream_t s) {
   const uint32_t parts = (uint32_t)((row_units<DT>(a) + LG_UNITS - 1) / LG_UNITS);
-  const int64_t all = a.rows, most = 4 * MAX_GROUPS / parts;   // V <= 2^30: at least 64
+  const int64_t all = a.rows, most = 4 * MAX_GROUPS / parts;   // V <= 2^30: at least 31
   for (int64_t done = 0; done < all; done += most) {
     a.rows = all - done < most ? all - done : most;
     const dim3 grid((unsigned)(a.rows * parts));

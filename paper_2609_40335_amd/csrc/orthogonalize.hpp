@@ -7,9 +7,9 @@
 // the diagonal are computed, and stored twice. So a step costs
 // m(m+1)n + m^2(m+1) + 2 m^2 n operations in three launches for the whole group. Bound by the
 // matrix cores, where launches have whole rounds of long tiles: GPT-2's 48 block matrices 98 us for A,
-// 43 for A^2 and 165 for the update (790 TFLOP/s), 205 to 245 where it carries X by itself (510 MB
-// more to move), 1.85 ms in five steps; 1601 x 6397 with two planes 104 us an update (950 TFLOP/s of
-// fp16 products), 1.0 ms in five steps.
+// 43 for A^2 and 168 for the update (780 TFLOP/s), 195 to 235 where it carries X by itself (510 MB
+// more to move), 1.87 ms in five steps; 1601 x 6397 with two planes 108 us an update (920 TFLOP/s of
+// fp16 products), 1.03 ms in five steps.
 //
 // The products run on the fp16 matrix cores. Singular values are at most about
 // 1.2 on the way, so that X, held as 2^12 X, and A and P, held as 2^10 A and
@@ -667,7 +667,7 @@ __global__ __launch_bounds__(256) void ns_join_kernel(NsArgs args) {
 // of a product. An update's blocks stay in registers until every wave has read Y. With one plane X's
 // blocks also stay there, in fp32, for as long as X goes into the update by itself (ns_fine).
 // Bound by latency: fifteen products in a row, each a barrier, a chain of LDS reads and the turn
-// through the slice. (Four matrices of a block of width 64, five steps, fp32 results: 41 us; in 17
+// through the slice. (Four matrices of a block of width 64, five steps, fp32 results: 43 us; in 17
 // launches of 5 to 9 us each 143.)
 template <int DT, int PL>
 __global__ __launch_bounds__(NS_SMALL_WAVES * WAVE) void ns_small_kernel(NsArgs args, NsCoefs coefs) {
