@@ -517,7 +517,7 @@ dp_status_t dp_clipped_grad_sum_positional_noised(const void* dE, int64_t lde, c
  * arrays of d elements of param_dt (NULL: 1 and 0). mean and rstd (fp32
  * [B*T], either may be NULL) are what the backward pass needs.
  * Statistics are fp32. d <= 32768 and B*T <= 2^31 - 2^16 (else DP_EUNSUPPORTED). Rows of
- * any alignment; operands may span more than 4 GiB.
+ * any alignment, of which nothing past d is read; operands may span more than 4 GiB.
  * ------------------------------------------------------------------- */
 dp_status_t dp_layernorm_forward(const void* x, int64_t ldx, const void* gain, const void* bias,
                                  dp_dtype_t param_dt, int B, int T, int d, dp_dtype_t dt,
@@ -555,8 +555,8 @@ dp_status_t dp_layernorm_backward(const void* gy, int64_t ldgy, const void* x, i
  * -inf logits have probability 0; a scored row of nothing else has logp = lse
  * = -inf and a zero gradient. NaN or +inf among a row's logits makes its
  * outputs NaN, which dp_clip_factors answers with c = 0.
- * V <= 2^30 and B*T <= 2^31 - 2^16 (else DP_EUNSUPPORTED); rows of any alignment;
- * operands may span more than 4 GiB.
+ * V <= 2^30 and B*T <= 2^31 - 2^16 (else DP_EUNSUPPORTED); rows of any alignment, of which nothing
+ * past V is read; operands may span more than 4 GiB.
  * ------------------------------------------------------------------- */
 /* logp [B,T] and (may be NULL) lse [B,T] (0 for rows that are not scored). */
 dp_status_t dp_token_logprobs(const void* Z, int64_t ldz, const int32_t* targets, int B, int T,

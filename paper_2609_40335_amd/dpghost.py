@@ -183,23 +183,14 @@ def _dtype(t: torch.Tensor) -> int:
     raise DPError(f"unsupported dtype {t.dtype}")
 
 
-def _row_stride(shape, st):
-    """The distance of a [B, T, w] view's token rows, None if it has no single one. With one
-    token an example that is the examples' distance (z[:, -1:, :], say)."""
-    B, T, w = shape
-    if st[2] != 1 or (B > 1 and T > 1 and st[0] != T * st[1]):
-        return None
-    return st[1] if T > 1 else st[0] if B > 1 else max(st[1], w)
-
-
 def _rows(t: torch.Tensor, name: str):
     """(pointer, B, T, width, row stride) of a token-major [B, T, w] tensor."""
     if t.dim() != 3:
         raise DPError(f"{name} must be [B, T, w]")
-    ld = _row_stride(t.shape, t.stride())
-    if ld is None:
+    B, T, w = t.shape
+    if t.stride(2) != 1 or (B > 1 and t.stride(0) != T * t.stride(1)):
         raise DPError(f"{name} must have unit feature stride and uniformly spaced token rows")
-    return (t.data_ptr(), *t.shape, ld)
+    return t.data_ptr(), B, T, w, t.stride(1)
 
 
 def _dev(t: torch.Tensor, name: str) -> None:
@@ -783,11 +774,15 @@ def _f32(t, shape, name: str):
 
 
 def _tokens(t, name: str):
-    """(pointer, [B, T, w], row stride) of a token-major tensor, as _rows checks it."""
+    """(pointer, [B, T, w], row stride) of a token-major tensor, as _rows checks it. With one
+    token an example the examples' distance is the row stride (z[:, -1:, :], say): LayerNorm and
+    the losses read no row past its width, so that the last one need not have room for it."""
     shape, st = t.shape, t.stride()
-    if len(shape) == 3 and st[2] == 1 and st[0] == shape[1] * st[1] and st[1] >= shape[2]:
-        return t.data_ptr(), shape, st[1]   # the common case, as cheap as it can be
-    return t.data_ptr(), shape, _rows(t, name)[4]
+    if len(shape) != 3 or st[2] != 1 or (shape[0] > 1 and st[0] != shape[1] * st[1]):
+        if len(shape) == 3 and st[2] == 1 and shape[1] == 1:
+            return t.data_ptr(), shape, st[0]
+        _rows(t, name)
+    return t.data_ptr(), shape, st[1]
 
 
 def _like(t, shape, dtype, name: str, of: str):

@@ -1,7 +1,8 @@
 """Views of token-major tensors as operands: what is one row stride, and what is not.
 
 The last token of every prompt, Z[:, -1:, :], is [B, 1, w] with rows T * ld apart: one row
-stride. All but the last, Z[:, :-1, :], has no single one."""
+stride. All but the last, Z[:, :-1, :], has no single one. The norms and sums, whose kernels may
+read a row, the last one too, up to its stride, refuse both."""
 import pytest
 
 from paper_2609_40335_amd import dpghost as D
@@ -9,9 +10,11 @@ from paper_2609_40335_amd import dpghost as D
 torch = pytest.importorskip("torch")
 
 
-@pytest.mark.parametrize("helper", [lambda t: D._tokens(t, "Z")[0::2],
-                                    lambda t: (lambda r: (r[0], r[4]))(D._rows(t, "Z"))])
-def test_row_stride_of_views(helper):
+def helper(t):
+    return D._tokens(t, "Z")[0::2]
+
+
+def test_row_stride_of_views():
     z = torch.zeros(3, 5, 8)
     buf = torch.zeros(3, 5, 16)
     for view, row, ld in ((z, 0, 8), (z[:, -1:, :], 4, 40), (buf[:, 2:3, :8], 2, 80), (buf[:, :, :8], 0, 16),
@@ -19,10 +22,11 @@ def test_row_stride_of_views(helper):
         p, got = helper(view)
         base = buf if view._base is buf else z
         assert got == ld and p == base.data_ptr() + row * base.shape[2] * 4, (view.shape, view.stride())
-    assert helper(torch.zeros(8).expand(1, 1, 8))[1] >= 8    # one row: its stride does not matter
     for view in (z[:, :-1, :], z[:, ::2, :], z[:, :, ::2], z.transpose(0, 1)):
         with pytest.raises(D.DPError, match="uniformly"):
             helper(view)
+    with pytest.raises(D.DPError, match="uniformly"):
+        D._rows(z[:, -1:, :], "Gz")
 
 
 def test_flattened_tokens_of_one_step():
@@ -50,11 +54,7 @@ def test_last_token_of_every_prompt(dt):
     dp.dp_cross_entropy(last, y, w, a, out[:, -1:, :])
     dp.dp_cross_entropy(last.contiguous(), y, w, b, want)
     assert torch.equal(out[:, -1:, :], want) and bool((out[:, :-1] == 5).all()) and torch.equal(a, b)
-    n, m = torch.empty(4, device="cuda"), torch.empty(4, device="cuda")
     h = torch.randn(4, 6, 40, device="cuda", generator=g).to(dt)
-    dp.dp_ghost_norm_linear(h[:, -1:, :], out[:, -1:, :], n)
-    dp.dp_ghost_norm_linear(h[:, -1:, :].contiguous(), want, m)
-    torch.testing.assert_close(n, m, rtol=2.0 ** -18, atol=0)   # other kernels where rows are aligned otherwise
     x, mean, rstd = torch.full_like(h, 5), torch.empty(4, 1, device="cuda"), torch.empty(4, 1, device="cuda")
     dp.dp_layernorm_forward(h[:, -1:, :], None, None, x[:, -1:, :], mean=mean, rstd=rstd)
     c = torch.empty(4, 1, 40, device="cuda", dtype=dt)
